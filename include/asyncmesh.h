@@ -294,6 +294,61 @@ am_status am_export_state(const am_state *st, am_snapshot *out);
 am_status am_resume_state(const am_config *cfg, const am_buffers *buf, void *hip_stream,
                           const am_snapshot *snapshot, am_state **out);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * The layers that own a stage's parameters, and the gradient norm.  They need no am_state: between two steps a training
+ * program takes weights out of the forward arrays, runs its layers, leaves gradients where am_step reads them and clips
+ * by a global norm.  Every call takes the R replicas in one go; replica i has its own weights and rows.
+ *
+ * Conventions beyond those at the top: work is enqueued on the stream given (NULL = the default stream) of the device that
+ * is current.  DEVICE pointers need the alignment of their elements only, because parameters lie at any place of a flat array;
+ * 16-byte aligned pointers and row strides are the fast case.  `workspace` (DEVICE, 256-byte aligned, at least the bytes that
+ * the matching *_workspace call names for the same arguments; NULL where it names 0) belongs to the call until the stream
+ * has passed it.  Outputs alias no input except where said.  Results do not depend on the order in which workgroups run.
+ * --------------------------------------------------------------------------------------------------------------------- */
+
+/* act(z): max(z, 0); z Phi(z); z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z)) */
+typedef enum { AM_ACT_NONE = 0, AM_ACT_RELU = 1, AM_ACT_GELU = 2, AM_ACT_GELU_TANH = 3, AM_ACT_SILU = 4 } am_act;
+
+typedef struct {
+    uint32_t replicas;       /* 1 .. AM_MAX_REPLICAS                                                      */
+    uint32_t dtype;          /* am_dtype of x, w, bias, residual, y, pre, dy, dx                          */
+    uint32_t grad_dtype;     /* am_dtype of dw, db (AM_BF16 only with dtype = AM_BF16)                    */
+    uint32_t act;            /* am_act                                                                    */
+    uint64_t rows;           /* M: rows (tokens) of x and y; 0: nothing is enqueued by am_linear, am_linear_backward clears dw, db */
+    uint64_t in, out;        /* K, N >= 1: w is [out][in], dense; rows, in and out below 2^31               */
+    uint64_t x_stride, y_stride, pre_stride, residual_stride, dx_stride;   /* elements from row to row (y_stride: of dy in the
+                                backward call); 0 = dense.  At least the row's length, below 2^31           */
+} am_linear_config;
+
+/* HOST arrays of `replicas` DEVICE pointers each; what a call does not use is ignored */
+typedef struct {
+    const void *const *x;         /* [rows][in]                                                          */
+    const void *const *w;         /* [out][in]                                                           */
+    const void *const *bias;      /* [out]; NULL: none                                                   */
+    const void *const *residual;  /* [rows][out], added after the activation; NULL: none; may be y itself */
+    void *const *y;               /* [rows][out]                                                         */
+    void *const *pre;             /* [rows][out] z: written by am_linear (NULL: not wanted), read by am_linear_backward
+                                     (needed with an activation, else ignored)                           */
+    const void *const *dy;        /* [rows][out]                                                         */
+    void *const *dx;              /* [rows][in]; NULL: not wanted                                        */
+    void *const *dw;              /* [out][in], dense; NULL: not wanted                                  */
+    void *const *db;              /* [out]; NULL: not wanted                                             */
+    void *workspace;
+    uint64_t workspace_bytes;
+} am_linear_buffers;
+
+/* Bytes of workspace am_linear (backward = 0) or am_linear_backward (1) needs for this config and these buffers (which
+ * outputs are wanted, and where the operands lie).  Host arithmetic only. */
+am_status am_linear_workspace(const am_linear_config *cfg, const am_linear_buffers *buf, int backward, uint64_t *out_bytes);
+
+/* y = act(z) + residual, z = x w^T + bias, for every replica; sums in fp32, every output rounded once. */
+am_status am_linear(const am_linear_config *cfg, const am_linear_buffers *buf, void *hip_stream);
+
+/* The gradients: dz = dy act'(z), dx = dz w, dw = dz^T x, db = column sums of dz.  act' is that of the stored z (relu' (0) = 0);
+ * with an activation, dz is rounded to dtype before the two products (db sums it unrounded).  accumulate != 0: dw and db are
+ * added to what is there (micro-batches), the sum rounded once.  The residual's gradient is dy itself. */
+am_status am_linear_backward(const am_linear_config *cfg, const am_linear_buffers *buf, int accumulate, void *hip_stream);
+
 am_status am_destroy(am_state *st);
 
 const char *am_last_error(void);      /* message of the last failing call on this thread */

@@ -14,13 +14,20 @@ _BINDING_NAMES = (
     "workspace_bytes",
 )
 
+_LAYER_NAMES = (
+    "ACT_NONE", "ACT_RELU", "ACT_GELU", "ACT_GELU_TANH", "ACT_SILU", "linear", "linear_backward",
+)
+
 
 def __getattr__(name):
     if name in _BINDING_NAMES:
         from . import binding
         return getattr(binding, name)
+    if name in _LAYER_NAMES:
+        from . import layers
+        return getattr(layers, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted(list(globals()) + list(_BINDING_NAMES))
+    return sorted(list(globals()) + list(_BINDING_NAMES) + list(_LAYER_NAMES))

@@ -1,4 +1,4 @@
-"""Builds libasyncmesh.so (the C-ABI HIP library) in-tree for gfx950 with hipcc.
+"""Builds libasyncmesh.so (the C-ABI HIP library) in-tree for gfx950 with hipcc, source files side by side.
 
 A digest of the library's source files is compiled into the library (am_version() ends with
 "src:<digest>"); `source_hash()` recomputes it from the files, so that tests, the smoke check and
@@ -8,12 +8,14 @@ from __future__ import annotations
 import hashlib
 import subprocess
 import sys
+import tempfile
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 SRC = PKG / "csrc" / "asyncmesh.hip"
-DEPS = [SRC, PKG / "csrc" / "am_kernels.h", PKG / "csrc" / "am_device.h", PKG / "csrc" / "am_geometry.h",
-        PKG / "csrc" / "am_host_logic.h", PKG.parent / "include" / "asyncmesh.h"]
+SOURCES = [SRC, *(PKG / "csrc" / f for f in ("am_linear.hip", "am_version.hip"))]
+DEPS = [*SOURCES, *(PKG / "csrc" / f for f in ("am_kernels.h", "am_device.h", "am_geometry.h", "am_host_logic.h", "am_error.h", "am_elem.h", "am_linear.h",
+                                               "am_product_plan.h")), PKG.parent / "include" / "asyncmesh.h"]
 LIB = PKG / "libasyncmesh.so"
 TEST_SRC = PKG.parent / "tests" / "list_kernel_driver.hip"      # kernels under launch parameters that only a test uses
 TEST_LIB = PKG.parent / "tests" / "liblist_kernel.so"
@@ -42,10 +44,16 @@ def stale() -> bool:
 
 def build_library(force: bool = True, verbose: bool = False) -> Path:
     if force or stale():
-        cmd = ["hipcc", *HIPCC_FLAGS, f'-DAM_SOURCE_HASH="{source_hash()}"', "-o", str(LIB), str(SRC)]
-        if verbose:
-            cmd.insert(1, "-Rpass-analysis=kernel-resource-usage")
-        subprocess.run(cmd, check=True)
+        define = f'-DAM_SOURCE_HASH="{source_hash()}"'
+        extra = ["-Rpass-analysis=kernel-resource-usage"] if verbose else []
+        with tempfile.TemporaryDirectory() as tmp:
+            objects = [Path(tmp) / (src.stem + ".o") for src in SOURCES]
+            compiles = [subprocess.Popen(["hipcc", *extra, *(f for f in HIPCC_FLAGS if f != "-shared"), define, "-c", "-o", str(obj), str(src)])
+                        for src, obj in zip(SOURCES, objects)]                       # (side by side)
+            failed = [src.name for src, job in zip(SOURCES, compiles) if job.wait() != 0]
+            if failed:
+                raise RuntimeError(f"hipcc failed on {', '.join(failed)}")
+            subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", str(LIB), *map(str, objects)], check=True)
     return LIB
 
 

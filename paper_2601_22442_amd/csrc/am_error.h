@@ -1,0 +1,19 @@
+// How a call reports what went wrong: the message of the calling thread, shared by the library's source files.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/asyncmesh.h"
+
+namespace am_host {
+// keeps the message for am_last_error and returns the status (asyncmesh.hip)
+__attribute__((visibility("hidden"), format(printf, 2, 3))) am_status fail(am_status code, const char *fmt, ...);
+
+inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+}  // namespace am_host
+
+#define AM_HIP(call)                                                                                    \
+    do {                                                                                                \
+        hipError_t e_ = (call);                                                                         \
+        if (e_ != hipSuccess) return am_host::fail(AM_EHIP, "%s: %s", #call, hipGetErrorString(e_));    \
+    } while (0)

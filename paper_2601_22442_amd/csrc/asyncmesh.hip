@@ -13,12 +13,9 @@
 #include <mutex>
 #include <new>
 
+#include "am_error.h"
 #include "am_host_logic.h"
 #include "am_kernels.h"
-
-#ifndef AM_SOURCE_HASH
-#define AM_SOURCE_HASH "unknown"
-#endif
 
 // Scratch of am_subset_indices_static: how many members each part of one subset has, for stages of up
 // to kStaticMaxN coordinates.  Every GPU the library runs on holds its own copy of
@@ -39,6 +36,9 @@ using am_host::Round;
 // allocates nothing and cannot throw
 thread_local char g_last_error[512] = "";
 
+}  // namespace
+
+namespace am_host {
 am_status fail(am_status code, const char *fmt, ...)
 {
     va_list ap;
@@ -47,14 +47,12 @@ am_status fail(am_status code, const char *fmt, ...)
     va_end(ap);
     return code;
 }
+}  // namespace am_host
 
-#define AM_HIP(call)                                                                          \
-    do {                                                                                      \
-        hipError_t e_ = (call);                                                               \
-        if (e_ != hipSuccess) return fail(AM_EHIP, "%s: %s", #call, hipGetErrorString(e_));   \
-    } while (0)
+namespace {
 
-inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+using am_host::aligned;
+using am_host::fail;
 
 constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mutex;
@@ -361,7 +359,6 @@ am_status fill_averaging(am_state *st, uint64_t t, float lambda_t, const Round &
 extern "C" {
 
 const char *am_last_error(void) { return g_last_error; }
-const char *am_version(void) { return "asyncmesh-gfx950 0.2 src:" AM_SOURCE_HASH; }
 
 am_status am_workspace_bytes(const am_config *cfg, uint64_t *out_bytes)
 {
