@@ -349,6 +349,70 @@ am_status am_linear(const am_linear_config *cfg, const am_linear_buffers *buf, v
  * added to what is there (micro-batches), the sum rounded once.  The residual's gradient is dy itself. */
 am_status am_linear_backward(const am_linear_config *cfg, const am_linear_buffers *buf, int accumulate, void *hip_stream);
 
+/* The gradients of a replica as the many tensors a training program has.  Every replica has the same ones. */
+typedef struct {
+    uint32_t replicas;            /* 1 .. AM_MAX_REPLICAS                                                   */
+    uint32_t tensors;             /* of each replica, 0 .. 2^20                                             */
+    const uint64_t *numel;        /* HOST, elements of each tensor, 0 allowed; together below 2^40           */
+    const uint32_t *dtype;        /* HOST, am_dtype of each tensor                                          */
+    uint32_t out_dtype;           /* am_dtype of the flat arrays                                            */
+    double max_norm;              /* >= 0 (infinity: never clipped)                                         */
+} am_norm_config;
+
+am_status am_norm_workspace(const am_norm_config *cfg, uint64_t *out_bytes);
+
+/* dev_norm[i] = sqrt(sum of squares over all of replica i's tensors), dev_factor[i] = 1 where the norm is at most max_norm, else
+ * max_norm / norm (DEVICE, R floats each; a NaN among the gradients makes both NaN; sums in fp64, fixed order).  dev_factor is what
+ * am_step_scaled takes.  grads: HOST array of replicas * tensors DEVICE pointers, replica after replica (a tensor without elements
+ * may be NULL).  out (NULL: none): HOST array of R DEVICE arrays that get the replica's gradients one after the other, in
+ * out_dtype, unscaled, in the same pass. */
+am_status am_grad_norm(const am_norm_config *cfg, const void *const *grads, void *const *out, float *dev_norm, float *dev_factor,
+                       void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
+/* The same norms and factors, and the gradients times their replica's factor, rounded once: into out, or with out = NULL in place. */
+am_status am_clip_grads(const am_norm_config *cfg, void *const *grads, void *const *out, float *dev_norm, float *dev_factor,
+                        void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
+/* Queries and keys before attention: every head is divided by its root mean square, multiplied by a gain, and its pairs are
+ * rotated by the position's angles, in one pass over memory. */
+typedef struct {
+    uint32_t replicas, dtype;     /* am_dtype of q, k, gains and what comes of them (dq, dk too)             */
+    uint32_t grad_dtype;          /* am_dtype of the gains' gradients (AM_BF16 only with dtype = AM_BF16)    */
+    uint32_t interleaved;         /* pairs of a head: 0: (j, j + rotated / 2), 1: (2 j, 2 j + 1)              */
+    uint64_t tokens;              /* T; 0: nothing is enqueued, backward clears the gains' gradients          */
+    uint32_t q_heads, k_heads;    /* 0 .. 65535, not both 0                                                   */
+    uint32_t head_dim;            /* D: even, 2 .. 512                                                        */
+    uint32_t rotated;             /* the first elements of a head that are rotated: even, 0 .. D              */
+    uint64_t q_stride, k_stride;  /* elements from token to token of q and k; heads lie side by side, D apart.  0 = dense; below 2^31 */
+    uint64_t table_rows;          /* rows of cos and sin                                                      */
+    double   eps;                 /* > 0: added to the mean square                                            */
+} am_qk_config;
+
+typedef struct {
+    /* HOST arrays of `replicas` DEVICE pointers */
+    const void *const *q, *const *k;              /* [tokens][heads][D]; not read where there are no such heads */
+    const void *const *q_gain, *const *k_gain;    /* [D]                                                      */
+    void *const *q_out, *const *k_out;            /* forward: [tokens][heads][D], dense                        */
+    const void *const *dq_out, *const *dk_out;    /* backward: the gradients of q_out and k_out, dense         */
+    void *const *dq, *const *dk;                  /* backward: dense                                           */
+    void *const *dq_gain, *const *dk_gain;        /* backward: [D]; NULL: not wanted                            */
+    const int32_t *const *positions;              /* [tokens], rows of the tables; a row that they do not have makes the token's rotated
+                                                     elements NaN.  NULL: token t has row t mod table_rows        */
+    const float *cos, *sin;                       /* DEVICE [table_rows][rotated / 2], the same for every replica and kept as they are */
+    void *workspace;
+    uint64_t workspace_bytes;
+} am_qk_buffers;
+
+/* Bytes of workspace am_qk_norm_backward needs (am_qk_norm: none) */
+am_status am_qk_norm_workspace(const am_qk_config *cfg, const am_qk_buffers *buf, uint64_t *out_bytes);
+
+/* n = x / sqrt(mean x^2 + eps), u = n gain, pair (a, b) of u -> (a cos - b sin, b cos + a sin); fp32 throughout, rounded once. */
+am_status am_qk_norm(const am_qk_config *cfg, const am_qk_buffers *buf, void *hip_stream);
+
+/* The gradients: du = the pairs turned back, dgain = sum over tokens and heads of du n, dx = (g du - n mean(g du n)) / sqrt(mean x^2 + eps).
+ * accumulate != 0: the gains' gradients are added to what is there.  Sums in fp32 in a fixed order, joined in fp64. */
+am_status am_qk_norm_backward(const am_qk_config *cfg, const am_qk_buffers *buf, int accumulate, void *hip_stream);
+
 am_status am_destroy(am_state *st);
 
 const char *am_last_error(void);      /* message of the last failing call on this thread */

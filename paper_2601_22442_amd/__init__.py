@@ -15,7 +15,7 @@ _BINDING_NAMES = (
 )
 
 _LAYER_NAMES = (
-    "ACT_NONE", "ACT_RELU", "ACT_GELU", "ACT_GELU_TANH", "ACT_SILU", "linear", "linear_backward",
+    "ACT_NONE", "ACT_RELU", "ACT_GELU", "ACT_GELU_TANH", "ACT_SILU", "linear", "linear_backward", "grad_norm", "clip_grads", "rotation_table", "qk_norm", "qk_norm_backward",
 )
 
 

@@ -29,6 +29,8 @@ EXPORTS = (
     "am_subset_indices", "am_subset_indices_static", "am_set_delay", "am_diagnostics", "am_read_flags", "am_set_profiling", "am_get_profile", "am_get_profile_times", "am_ring_info",
     "am_export_state", "am_resume_state",
     "am_linear_workspace", "am_linear", "am_linear_backward",
+    "am_norm_workspace", "am_grad_norm", "am_clip_grads",
+    "am_qk_norm_workspace", "am_qk_norm", "am_qk_norm_backward",
     "am_destroy", "am_last_error", "am_version",
 )
 

@@ -13,8 +13,8 @@ from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 SRC = PKG / "csrc" / "asyncmesh.hip"
-SOURCES = [SRC, *(PKG / "csrc" / f for f in ("am_linear.hip", "am_version.hip"))]
-DEPS = [*SOURCES, *(PKG / "csrc" / f for f in ("am_kernels.h", "am_device.h", "am_geometry.h", "am_host_logic.h", "am_error.h", "am_elem.h", "am_linear.h",
+SOURCES = [SRC, *(PKG / "csrc" / f for f in ("am_linear.hip", "am_norm.hip", "am_qk_norm.hip", "am_version.hip"))]
+DEPS = [*SOURCES, *(PKG / "csrc" / f for f in ("am_kernels.h", "am_device.h", "am_geometry.h", "am_host_logic.h", "am_error.h", "am_elem.h", "am_linear.h", "am_norm.h", "am_qk_norm.h",
                                                "am_product_plan.h")), PKG.parent / "include" / "asyncmesh.h"]
 LIB = PKG / "libasyncmesh.so"
 TEST_SRC = PKG.parent / "tests" / "list_kernel_driver.hip"      # kernels under launch parameters that only a test uses

@@ -14,8 +14,12 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 template <int ALIGN> struct __attribute__((packed, aligned(ALIGN))) Chunk16 { u32x4 v; };
 
+template <int ALIGN> struct __attribute__((packed, aligned(ALIGN))) Chunk8 { u32x2 v; };
+
 template <typename T> __device__ __forceinline__ u32x4 load16(const T *p) { return reinterpret_cast<const Chunk16<sizeof(T)> *>(p)->v; }
 template <typename T> __device__ __forceinline__ void store16(T *p, u32x4 v) { reinterpret_cast<Chunk16<sizeof(T)> *>(p)->v = v; }
+
+template <typename T> __device__ __forceinline__ void store8bytes(T *p, u32x2 v) { reinterpret_cast<Chunk8<sizeof(T)> *>(p)->v = v; }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }

@@ -1,0 +1,175 @@
+// Host side of am_grad_norm and am_clip_grads: argument checks, the cut into parts and launches.
+#include <cmath>
+#include <cstring>
+
+#include "am_error.h"
+#include "am_norm.h"
+
+namespace {
+
+using am_host::aligned;
+using am_host::fail;
+
+constexpr uint64_t kMaxElements = 1ull << 40;
+constexpr uint32_t kMaxTensors = 1u << 20;
+
+struct Cut {
+    uint32_t part_elements;
+    uint64_t parts;          // of a replica
+    uint64_t elements;
+};
+
+am_status check_config(const am_norm_config *c, Cut *cut)
+{
+    if (!c) return fail(AM_EINVAL, "config is NULL");
+    if (c->replicas == 0 || c->replicas > AM_MAX_REPLICAS) return fail(AM_EINVAL, "replicas=%u out of range [1, %u]", c->replicas, AM_MAX_REPLICAS);
+    if (c->tensors > kMaxTensors) return fail(AM_EINVAL, "tensors=%u out of range [0, %u]", c->tensors, kMaxTensors);
+    if (c->tensors && (!c->numel || !c->dtype)) return fail(AM_EINVAL, "numel / dtype is NULL");
+    if (c->out_dtype > AM_BF16) return fail(AM_EINVAL, "unknown out_dtype %u", c->out_dtype);
+    if (!(c->max_norm >= 0.)) return fail(AM_EINVAL, "max_norm=%g is negative or not a number", c->max_norm);
+    uint64_t all = 0;
+    for (uint32_t t = 0; t < c->tensors; ++t) {
+        if (c->dtype[t] > AM_BF16) return fail(AM_EINVAL, "unknown dtype[%u]=%u", t, c->dtype[t]);
+        if (c->numel[t] >= kMaxElements || (all += c->numel[t]) >= kMaxElements) return fail(AM_EINVAL, "the tensors have 2^40 elements or more");
+    }
+    // a part is 8192 elements, more where a replica would come to over 8192 parts
+    uint64_t part = 8192;
+    while (all / part > 8192u) part *= 2;
+    cut->part_elements = (uint32_t)part;
+    cut->parts = 0;
+    for (uint32_t t = 0; t < c->tensors; ++t) cut->parts += (c->numel[t] + part - 1) / part;
+    cut->elements = all;
+    return AM_OK;
+}
+
+am_status check_arrays(const am_norm_config &c, const Cut &cut, const void *const *grads, const void *const *out, const float *norm, const float *factor)
+{
+    if (c.tensors && !grads) return fail(AM_EINVAL, "grads is NULL");
+    if (!norm || !factor) return fail(AM_EINVAL, "dev_norm / dev_factor is NULL");
+    if (!aligned(norm, 4) || !aligned(factor, 4)) return fail(AM_EALIGN, "dev_norm / dev_factor is not 4-byte aligned");
+    for (uint32_t i = 0; i < c.replicas; ++i) {
+        for (uint32_t t = 0; t < c.tensors; ++t) {
+            const void *g = grads[(uint64_t)i * c.tensors + t];
+            if (c.numel[t] == 0) continue;
+            if (!g) return fail(AM_EINVAL, "grads of replica %u, tensor %u is NULL", i, t);
+            if (!aligned(g, c.dtype[t] == AM_BF16 ? 2 : 4)) return fail(AM_EALIGN, "grads of replica %u, tensor %u is not aligned to its elements", i, t);
+        }
+        if (out && !out[i] && cut.elements) return fail(AM_EINVAL, "out[%u] is NULL", i);
+        if (out && !aligned(out[i], c.out_dtype == AM_BF16 ? 2 : 4)) return fail(AM_EALIGN, "out[%u] is not aligned to its elements", i);
+    }
+    return AM_OK;
+}
+
+// Calls launch(table, parts of a replica in it) for as many tensors at a time as a launch's arguments hold.
+template <typename F>
+am_status each_table(const am_norm_config &c, const Cut &cut, const void *const *grads, void *const *out, F launch)
+{
+    uint32_t most = am::kNormPointers / c.replicas;
+    most = most < am::kNormTensors ? most : am::kNormTensors;
+    am::NormTable a;
+    uint32_t t = 0;
+    uint64_t at = 0, before = 0;
+    while (t < c.tensors) {
+        std::memset(&a, 0, sizeof a);
+        a.part_elements = cut.part_elements;
+        a.parts_before = (uint32_t)before; a.parts_all = (uint32_t)cut.parts;
+        a.out_bf16 = c.out_dtype == AM_BF16;
+        const void *source[am::kNormTensors][am::kNormMaxReplicas];
+        uint32_t k = 0, parts = 0;
+        for (; t < c.tensors && k < most; ++t) {
+            const uint64_t n = c.numel[t];
+            if (n == 0) continue;
+            a.first_part[k] = parts;
+            a.numel[k] = n;
+            a.at[k] = at;
+            if (c.dtype[t] == AM_BF16) a.bf16 |= 1ull << k;
+            for (uint32_t i = 0; i < c.replicas; ++i) source[k][i] = grads[(uint64_t)i * c.tensors + t];
+            parts += (uint32_t)((n + cut.part_elements - 1) / cut.part_elements);
+            at += n;
+            ++k;
+        }
+        if (k == 0) break;
+        a.first_part[k] = parts;
+        a.tensors = k;
+        for (uint32_t i = 0; i < c.replicas; ++i) {
+            if (out) a.out[i] = out[i];
+            for (uint32_t j = 0; j < k; ++j) a.g[i * k + j] = const_cast<void *>(source[j][i]);
+        }
+        launch(a, parts);
+        AM_HIP(hipGetLastError());
+        before += parts;
+    }
+    return AM_OK;
+}
+
+am_status norms(const am_norm_config &c, const Cut &cut, const void *const *grads, void *const *out, float *norm, float *factor, double *partial, hipStream_t stream)
+{
+    const am_status s = each_table(c, cut, grads, out, [&](const am::NormTable &a, uint32_t parts) {
+        const dim3 grid(parts, c.replicas);
+        if (!out) am::k_norm_parts<0><<<grid, am::kNormThreads, 0, stream>>>(a, partial);
+        else if (c.out_dtype == AM_F32) am::k_norm_parts<1><<<grid, am::kNormThreads, 0, stream>>>(a, partial);
+        else am::k_norm_parts<2><<<grid, am::kNormThreads, 0, stream>>>(a, partial);
+    });
+    if (s != AM_OK) return s;
+    am::k_norm_finish<<<c.replicas, am::kNormThreads, 0, stream>>>(partial, (uint32_t)cut.parts, c.max_norm, norm, factor);
+    AM_HIP(hipGetLastError());
+    return AM_OK;
+}
+
+am_status check_space(uint64_t need, const void *workspace, uint64_t bytes)
+{
+    if (need == 0) return AM_OK;
+    if (!workspace) return fail(AM_EINVAL, "workspace is NULL, %llu bytes needed", (unsigned long long)need);
+    if (!aligned(workspace, 256)) return fail(AM_EALIGN, "workspace is not 256-byte aligned");
+    if (bytes < need) return fail(AM_ENOMEM, "workspace has %llu bytes, %llu needed", (unsigned long long)bytes, (unsigned long long)need);
+    return AM_OK;
+}
+
+am_status prepare(const am_norm_config *cfg, const void *const *grads, void *const *out, const float *norm, const float *factor,
+                  const void *workspace, uint64_t bytes, Cut *cut)
+{
+    am_status s = check_config(cfg, cut);
+    if (s != AM_OK) return s;
+    s = check_arrays(*cfg, *cut, grads, const_cast<const void *const *>(out), norm, factor);
+    return s != AM_OK ? s : check_space(8u * cut->parts * cfg->replicas, workspace, bytes);
+}
+
+}  // namespace
+
+extern "C" {
+
+am_status am_norm_workspace(const am_norm_config *cfg, uint64_t *out_bytes)
+{
+    if (!out_bytes) return fail(AM_EINVAL, "out_bytes is NULL");
+    Cut cut;
+    const am_status s = check_config(cfg, &cut);
+    if (s != AM_OK) return s;
+    *out_bytes = 8u * cut.parts * cfg->replicas;
+    return AM_OK;
+}
+
+am_status am_grad_norm(const am_norm_config *cfg, const void *const *grads, void *const *out, float *dev_norm, float *dev_factor,
+                       void *workspace, uint64_t workspace_bytes, void *hip_stream)
+{
+    Cut cut;
+    const am_status s = prepare(cfg, grads, out, dev_norm, dev_factor, workspace, workspace_bytes, &cut);
+    if (s != AM_OK) return s;
+    return norms(*cfg, cut, grads, out, dev_norm, dev_factor, static_cast<double *>(workspace), static_cast<hipStream_t>(hip_stream));
+}
+
+am_status am_clip_grads(const am_norm_config *cfg, void *const *grads, void *const *out, float *dev_norm, float *dev_factor,
+                        void *workspace, uint64_t workspace_bytes, void *hip_stream)
+{
+    Cut cut;
+    const void *const *in = const_cast<const void *const *>(grads);
+    am_status s = prepare(cfg, in, out, dev_norm, dev_factor, workspace, workspace_bytes, &cut);
+    if (s != AM_OK) return s;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    s = norms(*cfg, cut, in, nullptr, dev_norm, dev_factor, static_cast<double *>(workspace), stream);
+    if (s != AM_OK) return s;
+    return each_table(*cfg, cut, in, out, [&](const am::NormTable &a, uint32_t parts) {
+        am::k_norm_scale<<<dim3(parts, cfg->replicas), am::kNormThreads, 0, stream>>>(a, dev_factor);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,204 @@
+// Host side of am_qk_norm and am_qk_norm_backward: argument checks, the lanes of a head, workspace and launches.
+#include <cmath>
+#include <cstring>
+
+#include "am_error.h"
+#include "am_qk_norm.h"
+
+namespace {
+
+using am_host::aligned;
+using am_host::fail;
+
+constexpr uint64_t kMaxExtent = 1ull << 31;
+
+am_status check_config(const am_qk_config *c)
+{
+    if (!c) return fail(AM_EINVAL, "config is NULL");
+    if (c->replicas == 0 || c->replicas > AM_MAX_REPLICAS) return fail(AM_EINVAL, "replicas=%u out of range [1, %u]", c->replicas, AM_MAX_REPLICAS);
+    if (c->dtype > AM_BF16 || c->grad_dtype > AM_BF16) return fail(AM_EINVAL, "unknown dtype");
+    if (c->dtype == AM_F32 && c->grad_dtype == AM_BF16) return fail(AM_EINVAL, "grad_dtype = bf16 needs dtype = bf16");
+    if (c->interleaved > 1) return fail(AM_EINVAL, "interleaved=%u is not 0 or 1", c->interleaved);
+    if (c->tokens >= kMaxExtent) return fail(AM_EINVAL, "tokens=%llu not below 2^31", (unsigned long long)c->tokens);
+    if (c->q_heads > 65535 || c->k_heads > 65535 || c->q_heads + c->k_heads == 0) return fail(AM_EINVAL, "q_heads=%u k_heads=%u out of range", c->q_heads, c->k_heads);
+    if (c->head_dim < 2 || c->head_dim > 512 || c->head_dim % 2) return fail(AM_EINVAL, "head_dim=%u is not an even number in [2, 512]", c->head_dim);
+    if (c->rotated > c->head_dim || c->rotated % 2) return fail(AM_EINVAL, "rotated=%u is not an even number up to head_dim=%u", c->rotated, c->head_dim);
+    if (c->table_rows >= kMaxExtent || (c->rotated && c->table_rows == 0)) return fail(AM_EINVAL, "table_rows=%llu out of range [1, 2^31)", (unsigned long long)c->table_rows);
+    if (!(c->eps > 0.) || !std::isfinite(c->eps) || (float)c->eps == 0.f) return fail(AM_EINVAL, "eps=%g is not a positive number", c->eps);
+    const struct { const char *name; uint64_t stride, heads; } strides[] = {{"q_stride", c->q_stride, c->q_heads}, {"k_stride", c->k_stride, c->k_heads}};
+    for (const auto &s : strides)
+        if (s.stride && (s.stride < s.heads * c->head_dim || s.stride >= kMaxExtent))
+            return fail(AM_EINVAL, "%s=%llu is shorter than a token's heads or not below 2^31", s.name, (unsigned long long)s.stride);
+    return AM_OK;
+}
+
+am_status check_table(const char *name, const void *const *p, const am_qk_config &c, uintptr_t align)
+{
+    if (!p) return fail(AM_EINVAL, "%s is NULL", name);
+    for (uint32_t i = 0; i < c.replicas; ++i) {
+        if (!p[i]) return fail(AM_EINVAL, "%s[%u] is NULL", name, i);
+        if (!aligned(p[i], align)) return fail(AM_EALIGN, "%s[%u] is not aligned to its elements", name, i);
+    }
+    return AM_OK;
+}
+
+#define AM_TABLE(name, align)                                                                                       \
+    do {                                                                                                            \
+        const am_status s_ = check_table(#name, reinterpret_cast<const void *const *>(buf->name), *cfg, align);     \
+        if (s_ != AM_OK) return s_;                                                                                 \
+    } while (0)
+
+am_status check(const am_qk_config *cfg, const am_qk_buffers *buf, bool backward)
+{
+    const am_status s = check_config(cfg);
+    if (s != AM_OK) return s;
+    if (!buf) return fail(AM_EINVAL, "buffers is NULL");
+    const uintptr_t size = cfg->dtype == AM_BF16 ? 2 : 4, gsize = cfg->grad_dtype == AM_BF16 ? 2 : 4;
+    if (backward && buf->dq_gain) AM_TABLE(dq_gain, gsize);
+    if (backward && buf->dk_gain) AM_TABLE(dk_gain, gsize);
+    if (cfg->tokens == 0) return AM_OK;
+    if (cfg->q_heads) {
+        AM_TABLE(q, size);
+        AM_TABLE(q_gain, size);
+        if (backward) { AM_TABLE(dq_out, size); AM_TABLE(dq, size); }
+        else AM_TABLE(q_out, size);
+    }
+    if (cfg->k_heads) {
+        AM_TABLE(k, size);
+        AM_TABLE(k_gain, size);
+        if (backward) { AM_TABLE(dk_out, size); AM_TABLE(dk, size); }
+        else AM_TABLE(k_out, size);
+    }
+    if (buf->positions) AM_TABLE(positions, 4);
+    if (cfg->rotated) {
+        if (!buf->cos || !buf->sin) return fail(AM_EINVAL, "cos / sin is NULL");
+        if (!aligned(buf->cos, 4) || !aligned(buf->sin, 4)) return fail(AM_EALIGN, "cos / sin is not 4-byte aligned");
+    }
+    return AM_OK;
+}
+
+// Eight pairs a lane where they lie in whole chunks, one otherwise; the lanes of a head are a power of two.
+struct Shape { int v, lanes, times; };
+Shape shape_of(const am_qk_config &c)
+{
+    const uint32_t pairs = c.head_dim / 2;
+    Shape s;
+    s.v = c.rotated / 2 % 8 == 0 && pairs % 8 == 0 ? 8 : 1;
+    const uint32_t units = pairs / (uint32_t)s.v;
+    s.lanes = 1;
+    while (s.lanes < 64 && (uint32_t)s.lanes < units) s.lanes *= 2;
+    s.times = (int)((units + (uint32_t)s.lanes - 1) / (uint32_t)s.lanes);
+    return s;
+}
+
+// Workgroups of a replica: some 2048 in all, no more than there are turns.
+uint32_t parts_of(const am_qk_config &c, const Shape &s)
+{
+    const uint64_t groups = am::kQkThreads / (uint32_t)s.lanes, turns = (c.tokens * (c.q_heads + c.k_heads) + groups - 1) / groups;
+    const uint64_t most = (2048 + c.replicas - 1) / c.replicas;
+    return (uint32_t)(turns < most ? turns : most);
+}
+
+uint64_t space(const am_qk_config &c, const am_qk_buffers &b)
+{
+    if (c.tokens == 0 || !((b.dq_gain && c.q_heads) || (b.dk_gain && c.k_heads))) return 0;
+    return 8ull * c.replicas * parts_of(c, shape_of(c)) * c.head_dim;
+}
+
+template <typename T, int V, int N, bool BACKWARD>
+void launch(const am::QkArgs &a, const am_qk_config &c, const Shape &s, hipStream_t stream)
+{
+    const uint32_t lds = BACKWARD && (a.want_gain[0] || a.want_gain[1]) ? am::kQkThreads / (uint32_t)s.lanes * c.head_dim * 4u : 0u;
+    am::k_qk_norm<T, V, N, BACKWARD><<<dim3(a.parts, c.replicas), am::kQkThreads, lds, stream>>>(a, s.lanes);
+}
+
+template <typename T, bool BACKWARD>
+am_status run(const am_qk_config &c, const am_qk_buffers &b, hipStream_t stream)
+{
+    am::QkArgs a;
+    std::memset(&a, 0, sizeof a);
+    for (uint32_t i = 0; i < c.replicas; ++i) {
+        if (c.q_heads) { a.x[0][i] = b.q[i]; a.gain[0][i] = b.q_gain[i]; a.out[0][i] = BACKWARD ? b.dq[i] : b.q_out[i]; if (BACKWARD) a.d[0][i] = b.dq_out[i]; }
+        if (c.k_heads) { a.x[1][i] = b.k[i]; a.gain[1][i] = b.k_gain[i]; a.out[1][i] = BACKWARD ? b.dk[i] : b.k_out[i]; if (BACKWARD) a.d[1][i] = b.dk_out[i]; }
+        if (b.positions) a.positions[i] = b.positions[i];
+    }
+    const Shape s = shape_of(c);
+    a.cos = b.cos; a.sin = b.sin;
+    a.stride[0] = c.q_stride ? c.q_stride : (uint64_t)c.q_heads * c.head_dim;
+    a.stride[1] = c.k_stride ? c.k_stride : (uint64_t)c.k_heads * c.head_dim;
+    a.tokens = (uint32_t)c.tokens; a.heads[0] = c.q_heads; a.heads[1] = c.k_heads; a.dim = c.head_dim; a.rotated = c.rotated;
+    a.interleaved = c.interleaved; a.rows = (uint32_t)c.table_rows; a.eps = (float)c.eps;
+    a.want_gain[0] = BACKWARD && b.dq_gain && c.q_heads; a.want_gain[1] = BACKWARD && b.dk_gain && c.k_heads;
+    a.parts = parts_of(c, s);
+    a.partial = static_cast<float *>(b.workspace);
+    if (s.v == 8) launch<T, 8, 1, BACKWARD>(a, c, s, stream);            // 32 lanes at most: 256 pairs
+    else if (s.times == 1) launch<T, 1, 1, BACKWARD>(a, c, s, stream);
+    else launch<T, 1, 4, BACKWARD>(a, c, s, stream);                    // 64 lanes, up to four pairs each
+    AM_HIP(hipGetLastError());
+    return AM_OK;
+}
+
+am_status gains(const am_qk_config &c, const am_qk_buffers &b, bool accumulate, hipStream_t stream)
+{
+    am::QkGainArgs g;
+    std::memset(&g, 0, sizeof g);
+    bool any = false;
+    for (uint32_t i = 0; i < c.replicas; ++i) {
+        if (b.dq_gain) g.dgain[0][i] = b.dq_gain[i];
+        if (b.dk_gain) g.dgain[1][i] = b.dk_gain[i];
+        any = b.dq_gain || b.dk_gain;
+    }
+    if (!any) return AM_OK;
+    const Shape s = shape_of(c);
+    g.partial = static_cast<const float *>(b.workspace);
+    g.parts = c.tokens ? parts_of(c, s) : 0u;
+    g.dim = c.head_dim; g.accumulate = accumulate;
+    const dim3 grid((c.head_dim + 15u) / 16u, 2, c.replicas);
+    if (c.grad_dtype == AM_F32) am::k_qk_gain<float><<<grid, 256, 0, stream>>>(g);
+    else am::k_qk_gain<__bf16><<<grid, 256, 0, stream>>>(g);
+    AM_HIP(hipGetLastError());
+    return AM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+am_status am_qk_norm_workspace(const am_qk_config *cfg, const am_qk_buffers *buf, uint64_t *out_bytes)
+{
+    if (!out_bytes) return fail(AM_EINVAL, "out_bytes is NULL");
+    const am_status s = check(cfg, buf, true);
+    if (s != AM_OK) return s;
+    *out_bytes = space(*cfg, *buf);
+    return AM_OK;
+}
+
+am_status am_qk_norm(const am_qk_config *cfg, const am_qk_buffers *buf, void *hip_stream)
+{
+    const am_status s = check(cfg, buf, false);
+    if (s != AM_OK || cfg->tokens == 0) return s;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    return cfg->dtype == AM_BF16 ? run<__bf16, false>(*cfg, *buf, stream) : run<float, false>(*cfg, *buf, stream);
+}
+
+am_status am_qk_norm_backward(const am_qk_config *cfg, const am_qk_buffers *buf, int accumulate, void *hip_stream)
+{
+    am_status s = check(cfg, buf, true);
+    if (s != AM_OK) return s;
+    // the gradient of a gain that no head uses is zero, like that of no tokens: the joining kernel must find no parts for it
+    if ((buf->dq_gain && !cfg->q_heads) || (buf->dk_gain && !cfg->k_heads)) return fail(AM_EINVAL, "the gradient of a gain without heads is wanted");
+    const uint64_t need = space(*cfg, *buf);
+    if (need) {
+        if (!buf->workspace) return fail(AM_EINVAL, "workspace is NULL, %llu bytes needed", (unsigned long long)need);
+        if (!aligned(buf->workspace, 256)) return fail(AM_EALIGN, "workspace is not 256-byte aligned");
+        if (buf->workspace_bytes < need) return fail(AM_ENOMEM, "workspace has %llu bytes, %llu needed", (unsigned long long)buf->workspace_bytes, (unsigned long long)need);
+    }
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (cfg->tokens) {
+        s = cfg->dtype == AM_BF16 ? run<__bf16, true>(*cfg, *buf, stream) : run<float, true>(*cfg, *buf, stream);
+        if (s != AM_OK) return s;
+    }
+    return gains(*cfg, *buf, accumulate != 0, stream);
+}
+
+}  // extern "C"

@@ -35,6 +35,33 @@ lib.am_linear.argtypes = [C.POINTER(LinearConfig), C.POINTER(LinearBuffers), C.c
 lib.am_linear_backward.argtypes = [C.POINTER(LinearConfig), C.POINTER(LinearBuffers), C.c_int, C.c_void_p]
 
 
+class NormConfig(C.Structure):
+    """Mirror of am_norm_config."""
+    _fields_ = [("replicas", C.c_uint32), ("tensors", C.c_uint32), ("numel", C.POINTER(C.c_uint64)), ("dtype", C.POINTER(C.c_uint32)),
+                ("out_dtype", C.c_uint32), ("max_norm", C.c_double)]
+
+
+class QkConfig(C.Structure):
+    """Mirror of am_qk_config."""
+    _fields_ = [("replicas", C.c_uint32), ("dtype", C.c_uint32), ("grad_dtype", C.c_uint32), ("interleaved", C.c_uint32), ("tokens", C.c_uint64),
+                ("q_heads", C.c_uint32), ("k_heads", C.c_uint32), ("head_dim", C.c_uint32), ("rotated", C.c_uint32),
+                ("q_stride", C.c_uint64), ("k_stride", C.c_uint64), ("table_rows", C.c_uint64), ("eps", C.c_double)]
+
+
+class QkBuffers(C.Structure):
+    """Mirror of am_qk_buffers."""
+    _fields_ = [(name, C.c_void_p) for name in ("q", "k", "q_gain", "k_gain", "q_out", "k_out", "dq_out", "dk_out", "dq", "dk", "dq_gain", "dk_gain",
+                                                "positions", "cos", "sin", "workspace")] + [("workspace_bytes", C.c_uint64)]
+
+
+lib.am_qk_norm_workspace.argtypes = [C.POINTER(QkConfig), C.POINTER(QkBuffers), C.POINTER(C.c_uint64)]
+lib.am_qk_norm.argtypes = [C.POINTER(QkConfig), C.POINTER(QkBuffers), C.c_void_p]
+lib.am_qk_norm_backward.argtypes = [C.POINTER(QkConfig), C.POINTER(QkBuffers), C.c_int, C.c_void_p]
+lib.am_norm_workspace.argtypes = [C.POINTER(NormConfig), C.POINTER(C.c_uint64)]
+for _f in (lib.am_grad_norm, lib.am_clip_grads):
+    _f.argtypes = [C.POINTER(NormConfig), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+
+
 def _replicas(name, tensors, count=None):
     tensors = list(tensors)
     if not 1 <= len(tensors) <= MAX_REPLICAS:
@@ -176,3 +203,166 @@ def linear_backward(dy, x, w, act=ACT_NONE, pre=None, dw=None, db=None, accumula
         tables["dx"] = _table(dx)
     _linear_call(cfg, tables, True, accumulate, device)
     return dx
+
+
+def _norm_call(entry, grads, max_norm, out):
+    grads = [list(g) for g in _replicas("grads", grads)]
+    R, count = len(grads), len(grads[0])
+    flat = [t for g in grads for t in g]
+    if len(flat) != R * count:
+        raise ValueError("grads: every replica must have the same tensors")
+    for name, tensors in (("grads", flat), ("out", [] if out is None else _replicas("out", out, R))):
+        for t in tensors:
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype in _DTYPES):
+                raise ValueError(f"{name} must hold contiguous float32 or bfloat16 tensors on a GPU")
+    if not flat and out is None:
+        raise ValueError("grads: no tensors")
+    device = flat[0].device if flat else out[0].device
+    index = device.index
+    sizes = [t.numel() for t in grads[0]]
+    types = [t.dtype for t in grads[0]]
+    for g in grads:
+        if [t.numel() for t in g] != sizes or [t.dtype for t in g] != types:
+            raise ValueError("grads: every replica must have the same tensors (number of elements and type)")
+    if any(t.get_device() != index for t in flat):
+        raise ValueError(f"grads: all tensors must be on {device}")
+    out_dtype, total = F32, sum(sizes)
+    if out is not None:
+        out = list(out)
+        out_dtype = _DTYPES[out[0].dtype]
+        for t in out:
+            if t.numel() != total or t.dtype != out[0].dtype or t.device != device:
+                raise ValueError(f"out must hold {R} tensors of {total} elements and one type on {device}")
+    cfg = NormConfig(R, count, (C.c_uint64 * count)(*sizes), (C.c_uint32 * count)(*[_DTYPES[t] for t in types]), out_dtype, max_norm)
+    pointers = _table(flat)
+    outs = None if out is None else _table(out)
+    result = torch.empty(2, R, dtype=torch.float32, device=device)
+    need = C.c_uint64(0)
+    with _on(device):
+        _check(lib.am_norm_workspace(C.byref(cfg), C.byref(need)))
+        space = _workspace(need.value, device)
+        at = result.data_ptr()
+        _check(entry(C.byref(cfg), pointers, outs, at, at + 4 * R, None if space is None else space.data_ptr(), need.value,
+                     torch.cuda.current_stream(device).cuda_stream))
+    return result[0], result[1]
+
+
+def grad_norm(grads, max_norm=float("inf"), out=None):
+    """The global norm of every replica's gradients and the factor that clips it to max_norm (am_grad_norm): grads is a list of R
+    lists of contiguous tensors, the same ones (sizes and types) for every replica.  out: R flat tensors that get the replica's gradients one after
+    the other, unscaled, in the same pass; with the factors as replica_scale that is what Stage.step_scaled takes.  Returns (norm, factor), device tensors of R floats."""
+    return _norm_call(lib.am_grad_norm, grads, max_norm, out)
+
+
+def clip_grads(grads, max_norm, out=None):
+    """Gradients times their replica's clipping factor (am_clip_grads), in place or into the flat tensors of out.  Returns (norm, factor), device tensors of R floats."""
+    return _norm_call(lib.am_clip_grads, grads, max_norm, out)
+
+
+def rotation_table(rows, rotated, base=10000.0, device="cuda:0"):
+    """(cos, sin) as qk_norm takes them: row p, pair j has the angle p base^(-2 j / rotated); fp32 [rows, rotated / 2], computed in fp64."""
+    rate = base ** (-torch.arange(0, rotated, 2, dtype=torch.float64, device=device) / max(rotated, 1))
+    angle = torch.arange(rows, dtype=torch.float64, device=device)[:, None] * rate
+    return angle.cos().float(), angle.sin().float()
+
+
+def _heads(name, tensors, tokens, heads, dim, dtype, device, dense=False):
+    """Checks [tokens, heads, dim] tensors; returns the stride from token to token that all replicas share (0: dense)."""
+    stride = None
+    for i, t in enumerate(tensors):
+        if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and tuple(t.shape) == (tokens, heads, dim)):
+            raise ValueError(f"{name}[{i}] must be a {dtype} tensor of shape {(tokens, heads, dim)} on {device}, got "
+                             f"{(tuple(t.shape), t.dtype, t.device) if isinstance(t, torch.Tensor) else type(t).__name__}")
+        if t.is_contiguous():
+            row = 0
+        elif dense or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (tokens > 1 and t.stride(0) < heads * dim):
+            raise ValueError(f"{name}[{i}] has strides {t.stride()}: " + ("it must be contiguous" if dense else "a token's heads must lie side by side"))
+        else:
+            row = t.stride(0) if tokens > 1 else 0
+        if stride is not None and row != stride:
+            raise ValueError(f"{name}: all replicas must have the same stride")
+        stride = row
+    return stride
+
+
+def _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
+    q = _replicas("q", q)
+    R = len(q)
+    k = _replicas("k", k, R)
+    device, dtype = _device_of("q", q[0]), q[0].dtype
+    if q[0].dim() != 3 or not isinstance(k[0], torch.Tensor) or k[0].dim() != 3:
+        raise ValueError("q and k must be lists of [tokens, heads, dim] tensors")
+    tokens, q_heads, dim = q[0].shape
+    k_heads = k[0].shape[1]
+    cfg = QkConfig(replicas=R, dtype=_DTYPES[dtype], grad_dtype=_DTYPES[dtype], interleaved=int(bool(interleaved)), tokens=tokens, q_heads=q_heads,
+                   k_heads=k_heads, head_dim=dim, eps=eps)
+    cfg.q_stride = _heads("q", q, tokens, q_heads, dim, dtype, device)
+    cfg.k_stride = _heads("k", k, tokens, k_heads, dim, dtype, device)
+    q_gain, k_gain = _replicas("q_gain", q_gain, R), _replicas("k_gain", k_gain, R)
+    _matching("q_gain", q_gain, (dim,), dtype, device, dense=True)
+    _matching("k_gain", k_gain, (dim,), dtype, device, dense=True)
+    if not (isinstance(cos, torch.Tensor) and isinstance(sin, torch.Tensor) and cos.dim() == 2 and cos.shape == sin.shape):
+        raise ValueError("cos and sin must be tensors of one shape [rows, rotated / 2]")
+    _matching("cos, sin", [cos, sin], tuple(cos.shape), torch.float32, device, dense=True)
+    cfg.table_rows, cfg.rotated = cos.shape[0], 2 * cos.shape[1]
+    buf, tables = QkBuffers(), {"q": _table(q), "k": _table(k), "q_gain": _table(q_gain), "k_gain": _table(k_gain)}
+    buf.cos, buf.sin = cos.data_ptr(), sin.data_ptr()
+    if positions is not None:
+        positions = _replicas("positions", positions, R)
+        _matching("positions", positions, (tokens,), torch.int32, device, dense=True)
+        tables["positions"] = _table(positions)
+    return cfg, buf, tables, device, dtype, tuple(q[0].shape), tuple(k[0].shape)
+
+
+def _fill(buf, tables):
+    for name, table in tables.items():
+        setattr(buf, name, C.addressof(table))
+
+
+def qk_norm(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, interleaved=False):
+    """Queries and keys of every replica before attention (am_qk_norm): each head divided by its root mean square, times a gain, its
+    pairs rotated.  Lists of R tensors: q [tokens, q heads, dim], k [tokens, k heads, dim], a token's heads side by side (views into the product
+    that made them); gains [dim]; cos and sin as rotation_table gives them (2 cos.shape[1] elements of a head are rotated: pairs
+    (j, j + half), interleaved (2 j, 2 j + 1)); positions int32 [tokens] rows of the tables, None: token mod rows, and a row that the tables do not
+    have makes the token NaN.  Returns two lists of dense tensors."""
+    cfg, buf, tables, device, dtype, q_shape, k_shape = _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
+    outs = [[torch.empty(shape, dtype=dtype, device=device) for _ in range(cfg.replicas)] for shape in (q_shape, k_shape)]
+    tables["q_out"], tables["k_out"] = _table(outs[0]), _table(outs[1])
+    _fill(buf, tables)
+    with _on(device):
+        _check(lib.am_qk_norm(C.byref(cfg), C.byref(buf), torch.cuda.current_stream(device).cuda_stream))
+    return outs[0], outs[1]
+
+
+def qk_norm_backward(dq, dk, q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, interleaved=False, dq_gain=None, dk_gain=None, accumulate=False):
+    """The gradients of qk_norm (am_qk_norm_backward): dq and dk are those of its two results (dense).  dq_gain and dk_gain [dim] are where the
+    gains' gradients go (None: not wanted), float32 or q's type; accumulate adds to what is there.  Returns the lists of the gradients of q and k."""
+    cfg, buf, tables, device, dtype, q_shape, k_shape = _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
+    dq, dk = _replicas("dq", dq, cfg.replicas), _replicas("dk", dk, cfg.replicas)
+    _heads("dq", dq, *q_shape, dtype, device, dense=True)
+    _heads("dk", dk, *k_shape, dtype, device, dense=True)
+    tables["dq_out"], tables["dk_out"] = _table(dq), _table(dk)
+    grad_dtype = None
+    for name, grads in (("dq_gain", dq_gain), ("dk_gain", dk_gain)):
+        if grads is None:
+            continue
+        grads = _replicas(name, grads, cfg.replicas)
+        if grad_dtype is None:
+            grad_dtype = grads[0].dtype
+            if grad_dtype not in (torch.float32, dtype):
+                raise ValueError(f"{name} must be float32 or {dtype}, not {grad_dtype}")
+        _matching(name, grads, (q_shape[2],), grad_dtype, device, dense=True)
+        tables[name] = _table(grads)
+    if grad_dtype is not None:
+        cfg.grad_dtype = _DTYPES[grad_dtype]
+    outs = [[torch.empty(shape, dtype=dtype, device=device) for _ in range(cfg.replicas)] for shape in (q_shape, k_shape)]
+    tables["dq"], tables["dk"] = _table(outs[0]), _table(outs[1])
+    _fill(buf, tables)
+    need = C.c_uint64(0)
+    with _on(device):
+        _check(lib.am_qk_norm_workspace(C.byref(cfg), C.byref(buf), C.byref(need)))
+        space = _workspace(need.value, device)
+        if space is not None:
+            buf.workspace, buf.workspace_bytes = space.data_ptr(), need.value
+        _check(lib.am_qk_norm_backward(C.byref(cfg), C.byref(buf), int(accumulate), torch.cuda.current_stream(device).cuda_stream))
+    return outs[0], outs[1]
