@@ -64,6 +64,7 @@ struct ProductArgs {
     const void *add[kLinearMaxReplicas];       // added after the activation, in C's type; all NULL: none (may be C itself)
     void *pre[kLinearMaxReplicas];             // z in the operands' type; all NULL: not kept
     uint32_t m, n, k;
+    uint32_t k_whole;                          // k rounded up to whole chunks where the operand that holds it side by side has zeros there, else k
     uint32_t lda, ldb, ldc, ldadd, ldpre;      // elements from row to row as the operands lie in memory
     uint32_t tiles_m, tiles_n, replicas;
     uint32_t act, out_f32;                     // activation; C and what is added are fp32 whatever the operands
@@ -127,7 +128,6 @@ __device__ __forceinline__ F8 bias8(const ProductArgs &p, uint32_t rep, uint32_t
 // operands
 // ---------------------------------------------------------------------------------------------
 template <typename T> constexpr int kChunk = 16 / (int)sizeof(T);       // elements of a chunk
-template <typename T> constexpr int kStep = 128 / (int)sizeof(T);       // k of a step: eight chunks
 
 // A chunk of which the first `valid` elements exist; the others read as 0.
 template <typename T> __device__ __forceinline__ u32x4 load_chunk(const T *p, int valid)
@@ -144,13 +144,16 @@ template <typename T> __device__ __forceinline__ u32x4 load_chunk(const T *p, in
     return r;
 }
 
-// One operand's part of a tile: R rows (m or n) by a step of k, brought in by NT threads.
-template <typename T, int R, int NT, bool ACROSS>
+static __device__ const u32x4 zero_chunk = {0u, 0u, 0u, 0u};
+
+// One operand's part of a tile: R rows (m or n) by a step of S chunks of k (eight or four), brought in by NT threads.
+template <typename T, int R, int NT, bool ACROSS, int S>
 struct Operand {
-    static constexpr int kPerThread = R * 8 / NT;
+    static constexpr int kStep = S * kChunk<T>;              // k of a step
+    static constexpr int kPerThread = R * S / NT;
     static constexpr int kRowChunks = R / kChunk<T>;
-    static constexpr int kBytes = R * 128;
-    static_assert(R * 8 % NT == 0, "chunks divide over the threads");
+    static constexpr int kBytes = R * S * 16;
+    static_assert(R * S % NT == 0 && (S == 8 || S == 4), "chunks divide over the threads");
 
     const T *base;
     uint64_t ld;
@@ -168,10 +171,11 @@ struct Operand {
             const int k = q / kRowChunks, c = q % kRowChunks;
             return (uint32_t)((k * kRowChunks + swizzle(k, c)) * 16);
         } else {
-            const int r = q / 8, c = q % 8;
-            return (uint32_t)((r * 8 + (c ^ (r & 7))) * 16);
+            const int r = q / S;
+            return (uint32_t)((r * S + turned(r, q % S)) * 16);
         }
     }
+    static __device__ __forceinline__ int turned(int r, int c) { return S == 8 ? c ^ (r & 7) : c ^ (r >> 1 & 3); }      // eight rows, 128 bytes of banks
     static __device__ __forceinline__ int swizzle(int k, int c)
     {
         if constexpr (sizeof(T) == 2) return c ^ ((k & 3) << 1);                 // a turned read takes two chunks of four neighbouring k
@@ -187,9 +191,41 @@ struct Operand {
                 const int k = q / kRowChunks, r = q % kRowChunks * kChunk<T>;
                 reg[i] = load_chunk(base + ((uint64_t)k0 + k) * ld + r, k < k_left ? rows_left - r : 0);
             } else {
-                const int r = q / 8, k = q % 8 * kChunk<T>;
+                const int r = q / S, k = q % S * kChunk<T>;
                 reg[i] = load_chunk(base + (uint64_t)r * ld + k0 + k, r < rows_left ? k_left - k : 0);
             }
+        }
+    }
+    // The same straight from memory into LDS, for operands in whole chunks (see direct_ok on the host): one wave's share of the
+    // chunks, in the order they have in LDS, so a lane asks for the chunk whose place is its own.  offset[]: bytes from
+    // base at k = 0, found once.  Rows past the end repeat the last ones (their products are not stored); chunks past the end of k are zeros.
+    __device__ __forceinline__ void offsets(uint32_t (&offset)[kPerThread], int wave, int lane) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+            const int q = (wave * kPerThread + i) * 64 + lane;
+            if constexpr (ACROSS) {
+                const int k = q / kRowChunks, r = swizzle(k, q % kRowChunks) * kChunk<T>, last = (rows_left - 1) / kChunk<T> * kChunk<T>;
+                offset[i] = (uint32_t)(k * (uint32_t)ld + (r < last ? r : last)) * (uint32_t)sizeof(T);
+            } else {
+                const int r = q / S, c = turned(r, q % S);
+                offset[i] = (uint32_t)((r < rows_left ? r : rows_left - 1) * (uint32_t)ld + c * kChunk<T>) * (uint32_t)sizeof(T);
+            }
+        }
+    }
+    __device__ __forceinline__ void direct(char *lds, const uint32_t (&offset)[kPerThread], uint32_t k0, int k_left, int wave, int lane) const
+    {
+        const char *from = reinterpret_cast<const char *>(base + (ACROSS ? (uint64_t)k0 * ld : (uint64_t)k0));
+        char *to = lds + wave * kPerThread * 1024;
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+            const char *at = from + offset[i];
+            if (k_left < kStep) {                 // (the last step alone)
+                const int q = (wave * kPerThread + i) * 64 + lane;
+                const int k = ACROSS ? q / kRowChunks : turned(q / S, q % S) * kChunk<T>;
+                at = k < k_left ? at : reinterpret_cast<const char *>(&zero_chunk);
+            }
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)at, (__attribute__((address_space(3))) void *)(to + i * 1024), 16, 0, 0);
         }
     }
     static __device__ __forceinline__ void keep(const u32x4 (&reg)[kPerThread], char *lds, int tid)
@@ -203,7 +239,7 @@ struct Operand {
     {
         const int i = lane & 15, g = lane >> 4;
         if constexpr (!ACROSS) {
-            return *reinterpret_cast<const u32x4 *>(lds + place((row + i) * 8 + h * 4 + g));
+            return *reinterpret_cast<const u32x4 *>(lds + place((row + i) * S + h * 4 + g));
         } else if constexpr (sizeof(T) == 2) {
             // lane i of sixteen reads four rows of k + i / 4 and gets four k of row i
             typedef __attribute__((address_space(3))) bf16x4 *lds_ptr;
@@ -254,91 +290,31 @@ __device__ __forceinline__ Where where(const ProductArgs &p, uint32_t block, uin
     return w;
 }
 
-// BM x BN tile, WM x WN waves, each BM / WM by BN / WN.  LDS: two steps of both operands, one read while the next is on its way
-// through registers; one barrier a step.
-template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS>
-__global__ void __launch_bounds__(64 * WM * WN, 2)
-k_product(const ProductArgs p)
+// The wave's sums (rows wm of the tile at m0, columns wn of that at n0) through its own part of LDS, at most 64 rows at a time, kept
+// [row][n] with chunks of four n moved by the row, then the epilogue.
+template <typename T, int ROWS, int COLS>
+__device__ __forceinline__ void finish_wave(const ProductArgs &p, const Where &w, f32x4 (&acc)[ROWS / 16][COLS / 16], char *lds, uint32_t m_first, uint32_t n_first, int wave, int lane)
 {
-    constexpr int NT = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
-    using A = Operand<T, BM, NT, A_ACROSS>;
-    using B = Operand<T, BN, NT, B_ACROSS>;
-    constexpr int kStage = A::kBytes + B::kBytes;
-    extern __shared__ __align__(16) char lds[];
-
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Where w = where(p, blockIdx.x, gridDim.x);
-    const uint32_t m0 = w.tile_m * BM, n0 = w.tile_n * BN;
-    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-    const uint32_t k_first = w.split * p.split_k;
-    const uint32_t k_end = p.k - k_first < p.split_k ? p.k : k_first + p.split_k;
-    const int steps = (int)((k_end - k_first + kStep<T> - 1) / kStep<T>);
-
-    A a;
-    B b;
-    a.init(p.a[w.replica], p.lda, m0, p.m);
-    b.init(p.b[w.replica], p.ldb, n0, p.n);
-    f32x4 acc[MF][NF];
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    u32x4 ra[A::kPerThread], rb[B::kPerThread];
-    a.load(ra, k_first, (int)(k_end - k_first), tid);
-    b.load(rb, k_first, (int)(k_end - k_first), tid);
-    A::keep(ra, lds, tid);
-    B::keep(rb, lds + A::kBytes, tid);
-    for (int t = 0; t < steps; ++t) {
-        __syncthreads();              // step t is in LDS, and nobody reads the other half any more
-        const char *cur = lds + (t & 1) * kStage;
-        if (t + 1 < steps) {
-            const uint32_t k0 = k_first + (uint32_t)(t + 1) * kStep<T>;
-            a.load(ra, k0, (int)(k_end - k0), tid);
-            b.load(rb, k0, (int)(k_end - k0), tid);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            u32x4 fa[MF], fb[NF];
-#pragma unroll
-            for (int j = 0; j < NF; ++j) fb[j] = B::fragment(cur + A::kBytes, wn + j * 16, h, lane);
-#pragma unroll
-            for (int i = 0; i < MF; ++i) fa[i] = A::fragment(cur, wm + i * 16, h, lane);
-#pragma unroll
-            for (int i = 0; i < MF; ++i)
-#pragma unroll
-                for (int j = 0; j < NF; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
-        }
-        if (t + 1 < steps) {
-            char *next = lds + ((t + 1) & 1) * kStage;
-            A::keep(ra, next, tid);
-            B::keep(rb, next + A::kBytes, tid);
-        }
-    }
-
-    // The wave's sums through its own part of LDS, at most 64 rows at a time: [row][n], chunks of four n moved by the row.
-    constexpr int kRows = BM / WM < 64 ? BM / WM : 64, kCols = BN / WN, kLanesARow = kCols / 8;
-    static_assert(kRows * kCols * 4 * WM * WN <= 2 * kStage, "the sums fit");
+    constexpr int kRows = ROWS < 64 ? ROWS : 64, kCols = COLS, kLanesARow = kCols / 8;
     char *mine = lds + wave * (kRows * kCols * 4);
     const int col = lane % kLanesARow * 8;
-    const uint32_t n = n0 + (uint32_t)(wn + col);
+    const uint32_t n = n_first + (uint32_t)col;
     const int valid = n >= p.n ? 0 : p.n - n < 8u ? (int)(p.n - n) : 8;
     const bool whole = p.splits <= 1u;
     const F8 bias = whole ? bias8<T>(p, w.replica, n, valid) : F8{};
-    __syncthreads();
 #pragma unroll
-    for (int part = 0; part < BM / WM / kRows; ++part) {
+    for (int part = 0; part < ROWS / kRows; ++part) {
 #pragma unroll
         for (int i = 0; i < kRows / 16; ++i)
 #pragma unroll
-            for (int j = 0; j < NF; ++j) {
+            for (int j = 0; j < COLS / 16; ++j) {
                 const int row = i * 16 + (lane & 15), c = j * 4 + (lane >> 4);
                 *reinterpret_cast<f32x4 *>(mine + (row * (kCols / 4) + (c ^ (row & (kCols / 4 - 1)))) * 16) = acc[part * (kRows / 16) + i][j];
             }
         // (one wave's LDS accesses are done in order)
 #pragma unroll 1
         for (int row = lane / kLanesARow; row < kRows; row += 64 / kLanesARow) {
-            const uint32_t m = m0 + (uint32_t)(wm + part * kRows + row);
+            const uint32_t m = m_first + (uint32_t)(part * kRows + row);
             if (m >= p.m || valid == 0) continue;
             F8 x;
 #pragma unroll
@@ -351,6 +327,213 @@ k_product(const ProductArgs p)
             else store8(p.partial + (((uint64_t)w.split * p.replicas + w.replica) * p.m + m) * p.n + n, valid, x);
         }
     }
+}
+
+// A step's products of one wave: cur holds the step, and what `ahead` writes meanwhile lies elsewhere in LDS.
+template <typename T, typename A, typename B, int MF, int NF>
+__device__ __forceinline__ void products(const char *__restrict__ cur, f32x4 (&acc)[MF][NF], int wm, int wn, int lane)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        u32x4 fa[MF], fb[NF];
+#pragma unroll
+        for (int j = 0; j < NF; ++j) fb[j] = B::fragment(cur + A::kBytes, wn + j * 16, h, lane);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) fa[i] = A::fragment(cur, wm + i * 16, h, lane);
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+    }
+}
+
+// The next step's chunks set out for `next`, then the products of the step in `cur`.
+template <typename T, typename A, typename B, int MF, int NF>
+__device__ __forceinline__ void direct_step(const char *__restrict__ cur, char *__restrict__ next, const A &a, const B &b,
+                                            const uint32_t (&oa)[A::kPerThread], const uint32_t (&ob)[B::kPerThread], uint32_t k0, int ka, int kb,
+                                            bool more, f32x4 (&acc)[MF][NF], int wm, int wn, int wave, int lane)
+{
+    if (more) {
+        a.direct(next, oa, k0, ka, wave, lane);
+        b.direct(next + A::kBytes, ob, k0, kb, wave, lane);
+    }
+    products<T, A, B, MF, NF>(cur, acc, wm, wn, lane);
+}
+
+// BM x BN tile, WM x WN waves, each BM / WM by BN / WN.  LDS: two steps of both operands, one read while the next is on its way
+// (DIRECT: straight from memory, else through registers); one barrier a step.
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN, 2)
+k_product(const ProductArgs p)
+{
+    constexpr int NT = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
+    using A = Operand<T, BM, NT, A_ACROSS, 8>;
+    using B = Operand<T, BN, NT, B_ACROSS, 8>;
+    constexpr int kStep = A::kStep;
+    constexpr int kStage = A::kBytes + B::kBytes;
+    extern __shared__ __align__(16) char lds[];
+
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Where w = where(p, blockIdx.x, gridDim.x);
+    const uint32_t m0 = w.tile_m * BM, n0 = w.tile_n * BN;
+    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+    const uint32_t k_first = w.split * p.split_k;
+    const uint32_t k_end = p.k - k_first < p.split_k ? p.k : k_first + p.split_k;
+    const int steps = (int)((k_end - k_first + kStep - 1) / kStep);
+
+    A a;
+    B b;
+    a.init(p.a[w.replica], p.lda, m0, p.m);
+    b.init(p.b[w.replica], p.ldb, n0, p.n);
+    f32x4 acc[MF][NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    if constexpr (DIRECT) {
+        uint32_t oa[A::kPerThread], ob[B::kPerThread];
+        a.offsets(oa, wave, lane);
+        b.offsets(ob, wave, lane);
+        // k_end is that of k as it is summed; an operand that holds k side by side has zeros up to a whole chunk
+        const int extra = (int)(p.k_whole - p.k);
+        int left = (int)(k_end - k_first);
+        const auto ends = [&](int l, bool across) { return across ? l : l + extra; };
+        a.direct(lds, oa, k_first, ends(left, A_ACROSS), wave, lane);
+        b.direct(lds + A::kBytes, ob, k_first, ends(left, B_ACROSS), wave, lane);
+        for (int t = 0; t < steps; ++t) {
+            __syncthreads();              // step t has come, and nobody reads the other half any more
+            left -= kStep;
+            direct_step<T, A, B, MF, NF>(lds + (t & 1) * kStage, lds + ((t + 1) & 1) * kStage, a, b, oa, ob, k_first + (uint32_t)(t + 1) * kStep,
+                                         ends(left, A_ACROSS), ends(left, B_ACROSS), t + 1 < steps, acc, wm, wn, wave, lane);
+        }
+    } else {
+        u32x4 ra[A::kPerThread], rb[B::kPerThread];
+        a.load(ra, k_first, (int)(k_end - k_first), tid);
+        b.load(rb, k_first, (int)(k_end - k_first), tid);
+        A::keep(ra, lds, tid);
+        B::keep(rb, lds + A::kBytes, tid);
+        for (int t = 0; t < steps; ++t) {
+            __syncthreads();              // step t is in LDS, and nobody reads the other half any more
+            if (t + 1 < steps) {
+                const uint32_t k0 = k_first + (uint32_t)(t + 1) * kStep;
+                a.load(ra, k0, (int)(k_end - k0), tid);
+                b.load(rb, k0, (int)(k_end - k0), tid);
+            }
+            products<T, A, B, MF, NF>(lds + (t & 1) * kStage, acc, wm, wn, lane);
+            if (t + 1 < steps) {
+                char *next = lds + ((t + 1) & 1) * kStage;
+                A::keep(ra, next, tid);
+                B::keep(rb, next + A::kBytes, tid);
+            }
+        }
+    }
+
+    __syncthreads();
+    static_assert(BM / WM * (BN / WN) * 4 * NT / 64 / (BM / WM > 64 ? BM / WM / 64 : 1) <= 2 * kStage, "the sums fit");
+    finish_wave<T, BM / WM, BN / WN>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
+}
+
+// The 256 x 256 tile of bf16, eight waves of 128 x 64 each, two to a SIMD: while one of the two multiplies, the other reads its
+// next fragments from LDS and sets out loads.  Steps of 64 bytes of k in four stages of LDS.  The waves of the second group of
+// four run half a step behind: between two barriers group 0 does memory for step q (interval 2q), then products (2q + 1); group 1
+// memory in 2q + 1, products in 2q + 2.  What the barriers then promise:
+//   step q is read in intervals 2q and 2q + 1, and the reads are over by the end of 2q + 2 (a wave's products wait for them);
+//   group 0 sets out step q + 2 in interval 2q, over step q - 2, read until 2q - 2; group 1 sets out its share of step q + 3 in
+//   2q + 1, over step q - 1, read until 2q;
+//   step q + 1 must be there before interval 2q + 2: group 0 waits for its share at the end of 2q + 1, when steps q + 1 and q + 2
+//   are on their way, group 1 at the end of 2q + 1 too, with q + 1, q + 2 and q + 3 on their way.
+// Steps past the end set out zeros, so that the counts stay.
+__device__ __forceinline__ void meet()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+template <int COUNT> __device__ __forceinline__ void wait_loads()      // until at most COUNT vector memory accesses of the wave are on their way
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
+}
+
+template <typename A, typename B, int MF, int NF>
+__device__ __forceinline__ void large_fetch(const char *__restrict__ cur, char *__restrict__ ahead, const A &a, const B &b, const uint32_t (&oa)[A::kPerThread],
+                                            const uint32_t (&ob)[B::kPerThread], uint32_t k0, int ka, int kb, u32x4 (&fa)[MF], u32x4 (&fb)[NF], int wm, int wn, int wave, int lane)
+{
+#pragma unroll
+    for (int j = 0; j < NF; ++j) fb[j] = B::fragment(cur + A::kBytes, wn + j * 16, 0, lane);
+#pragma unroll
+    for (int i = 0; i < MF; ++i) fa[i] = A::fragment(cur, wm + i * 16, 0, lane);
+    a.direct(ahead, oa, k0, ka, wave, lane);
+    b.direct(ahead + A::kBytes, ob, k0, kb, wave, lane);
+}
+
+template <bool A_ACROSS, bool B_ACROSS>
+__global__ void __launch_bounds__(512, 2)
+k_product_large(const ProductArgs p)
+{
+    typedef __bf16 T;
+    constexpr int BM = 256, BN = 256, NT = 512, MF = 8, NF = 4;
+    using A = Operand<T, BM, NT, A_ACROSS, 4>;
+    using B = Operand<T, BN, NT, B_ACROSS, 4>;
+    constexpr int kStep = A::kStep, kStage = A::kBytes + B::kBytes, kLoads = A::kPerThread + B::kPerThread;
+    extern __shared__ __align__(16) char lds[];
+
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = wave >> 2;
+    const Where w = where(p, blockIdx.x, gridDim.x);
+    const uint32_t m0 = w.tile_m * BM, n0 = w.tile_n * BN;
+    const int wm = wave / 4 * 128, wn = wave % 4 * 64;
+    const uint32_t k_first = w.split * p.split_k;
+    const uint32_t k_end = p.k - k_first < p.split_k ? p.k : k_first + p.split_k;
+    const int steps = (int)((k_end - k_first + kStep - 1) / kStep);
+
+    A a;
+    B b;
+    a.init(p.a[w.replica], p.lda, m0, p.m);
+    b.init(p.b[w.replica], p.ldb, n0, p.n);
+    uint32_t oa[A::kPerThread], ob[B::kPerThread];
+    a.offsets(oa, wave, lane);
+    b.offsets(ob, wave, lane);
+    f32x4 acc[MF][NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const int extra = (int)(p.k_whole - p.k), all = (int)(k_end - k_first);
+    const auto set_out = [&](int step) {
+        char *to = lds + (step & 3) * kStage;
+        const uint32_t k0 = step < steps ? k_first + (uint32_t)step * kStep : k_first;      // (past the end: no address of it is used)
+        const int left = all - step * kStep;
+        a.direct(to, oa, k0, A_ACROSS ? left : left + extra, wave, lane);
+        b.direct(to + A::kBytes, ob, k0, B_ACROSS ? left : left + extra, wave, lane);
+    };
+    set_out(0);
+    set_out(1);
+    if (group) { set_out(2); wait_loads<2 * kLoads>(); }
+    else wait_loads<kLoads>();
+    meet();
+    if (group) meet();
+    for (int q = 0; q < steps; ++q) {
+        u32x4 fa[MF], fb[NF];
+        const int s = q + 2 + group, left = all - s * kStep;
+        const uint32_t k0 = s < steps ? k_first + (uint32_t)s * kStep : k_first;
+        large_fetch<A, B, MF, NF>(lds + (q & 3) * kStage, lds + (s & 3) * kStage, a, b, oa, ob, k0, A_ACROSS ? left : left + extra, B_ACROSS ? left : left + extra,
+                                  fa, fb, wm, wn, wave, lane);
+        if (group) wait_loads<2 * kLoads>();
+        meet();
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+        __builtin_amdgcn_s_setprio(0);
+        if (!group) wait_loads<kLoads>();
+        meet();
+    }
+    if (!group) meet();
+    wait_loads<0>();
+    __syncthreads();
+    finish_wave<T, 128, 64>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
 }
 
 // The parts of k that workgroups summed apart, joined in their order, and the epilogue.
@@ -400,7 +583,7 @@ k_columns(const ColumnArgs p)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d.v[j] *= act_grad_f32<ACT>(z.v[j]);
             }
-            if (p.dz[rep]) store8(static_cast<T *>(p.dz[rep]) + (uint64_t)m * p.lddz + n, valid, d);
+            if (p.dz[rep]) store8(static_cast<T *>(p.dz[rep]) + (uint64_t)m * p.lddz + n, 8, d);       // (rows are padded to eight with zeros)
             add8(acc, d);
         }
     }

@@ -132,37 +132,56 @@ am_status check_space(const am_linear_buffers *buf, uint64_t need)
 }
 
 // ---- launches -------------------------------------------------------------------------------
-template <typename T, int BM, int BN, int WM, int WN, bool AA, bool BA>
-am_status launch_tiles(ProductArgs &a, hipStream_t stream)
+am_status launch_kernel(void (*kernel)(ProductArgs), ProductArgs &a, uint32_t tile, uint32_t threads, uint32_t lds, hipStream_t stream)
 {
-    a.tiles_m = (a.m + BM - 1) / BM;
-    a.tiles_n = (a.n + BN - 1) / BN;
+    a.tiles_m = (a.m + tile - 1) / tile;
+    a.tiles_n = (a.n + tile - 1) / tile;
     const uint64_t blocks = (uint64_t)a.tiles_m * a.tiles_n * a.replicas * a.splits;
     if (blocks >= kMaxExtent) return fail(AM_EINVAL, "a product of %llu tiles is too large for one launch", (unsigned long long)blocks);
-    constexpr uint32_t lds = 2u * (BM + BN) * 128u;
-    const auto kernel = am::k_product<T, BM, BN, WM, WN, AA, BA>;
-    AM_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    kernel<<<(uint32_t)blocks, 64 * WM * WN, lds, stream>>>(a);
+    if (lds > 65536u) AM_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    kernel<<<(uint32_t)blocks, threads, lds, stream>>>(a);
     AM_HIP(hipGetLastError());
     return AM_OK;
 }
 
-template <typename T, bool AA, bool BA>
+template <typename T, int BM, int BN, int WM, int WN, bool AA, bool BA, bool DIRECT>
+am_status launch_tiles(ProductArgs &a, hipStream_t stream)
+{
+    static_assert(BM == BN, "square tiles");
+    return launch_kernel(am::k_product<T, BM, BN, WM, WN, AA, BA, DIRECT>, a, BM, 64 * WM * WN, 2u * (BM + BN) * 128u, stream);
+}
+
+template <typename T, bool AA, bool BA, bool DIRECT>
 am_status launch_shape(ProductArgs &a, const ProductPlan &p, hipStream_t stream)
 {
-    if constexpr (sizeof(T) == 2)
-        if (p.tile == 256) return launch_tiles<T, 256, 256, 2, 4, AA, BA>(a, stream);
-    if (p.tile == 64) return launch_tiles<T, 64, 64, 2, 2, AA, BA>(a, stream);
-    return launch_tiles<T, 128, 128, 2, 2, AA, BA>(a, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (p.tile == 256) {
+            if constexpr (DIRECT) return launch_kernel(am::k_product_large<AA, BA>, a, 256, 512, 131072, stream);
+            else return launch_tiles<T, 256, 256, 2, 4, AA, BA, DIRECT>(a, stream);
+        }
+    }
+    if (p.tile == 64) return launch_tiles<T, 64, 64, 2, 2, AA, BA, DIRECT>(a, stream);
+    return launch_tiles<T, 128, 128, 2, 2, AA, BA, DIRECT>(a, stream);
+}
+
+// Whether an operand can be read straight into LDS: whole chunks of 16 bytes, aligned, and an offset within a tile that fits 32 bits.
+// side: the length of its rows in memory (k, or across the tile's rows).
+template <typename T>
+bool in_chunks(const void *const *p, uint32_t replicas, uint64_t ld, uint64_t side)
+{
+    constexpr uint64_t chunk = 16 / sizeof(T);
+    bool ok = ld % chunk == 0 && side % chunk == 0 && ld < (1ull << 22);
+    for (uint32_t i = 0; i < replicas; ++i) ok = ok && aligned(p[i], 16);
+    return ok;
 }
 
 template <typename T, bool AA, bool BA>
-am_status launch_product(ProductArgs &a, const ProductPlan &p, float *partial, hipStream_t stream)
+am_status launch_product(ProductArgs &a, const ProductPlan &p, bool direct, float *partial, hipStream_t stream)
 {
     a.splits = p.splits;
     a.split_k = p.split_k;
     a.partial = partial;
-    const am_status s = launch_shape<T, AA, BA>(a, p, stream);
+    const am_status s = direct ? launch_shape<T, AA, BA, true>(a, p, stream) : launch_shape<T, AA, BA, false>(a, p, stream);
     if (s != AM_OK || p.splits <= 1) return s;
     const uint64_t blocks = ((uint64_t)((a.n + 7u) / 8u) * a.m + 255u) / 256u;
     am::k_product_join<T><<<dim3((uint32_t)(blocks < 4096u ? blocks : 4096u), 1, a.replicas), 256, 0, stream>>>(a);
@@ -187,7 +206,9 @@ am_status forward(const am_linear_config &c, const am_linear_buffers &b, hipStre
     a.act = c.act;
     a.lda = (uint32_t)or_dense(c.x_stride, c.in); a.ldb = (uint32_t)c.in; a.ldc = (uint32_t)or_dense(c.y_stride, c.out);
     a.ldadd = (uint32_t)or_dense(c.residual_stride, c.out); a.ldpre = (uint32_t)or_dense(c.pre_stride, c.out);
-    return launch_product<T, false, false>(a, plan_product(c, kRows), static_cast<float *>(b.workspace), stream);
+    a.k_whole = a.k;
+    const bool direct = in_chunks<T>(a.a, c.replicas, a.lda, a.k) && in_chunks<T>(a.b, c.replicas, a.ldb, a.k);
+    return launch_product<T, false, false>(a, plan_product(c, kRows), direct, static_cast<float *>(b.workspace), stream);
 }
 
 template <typename T, int ACT>
@@ -264,7 +285,9 @@ am_status backward(const am_linear_config &c, const am_linear_buffers &b, const 
         for (uint32_t i = 0; i < c.replicas; ++i) { a.b[i] = b.w[i]; a.c[i] = b.dx[i]; }
         a.m = (uint32_t)c.rows; a.n = (uint32_t)c.in; a.k = (uint32_t)c.out;
         a.lda = lddz; a.ldb = (uint32_t)c.in; a.ldc = (uint32_t)or_dense(c.dx_stride, c.in);
-        const am_status s = launch_product<T, false, true>(a, plan_product(c, kInputGradient), partial, stream);
+        a.k_whole = own_dz ? (uint32_t)sp.dz_pitch : a.k;
+        const bool direct = in_chunks<T>(a.a, c.replicas, a.lda, a.k_whole) && in_chunks<T>(a.b, c.replicas, a.ldb, a.n);
+        const am_status s = launch_product<T, false, true>(a, plan_product(c, kInputGradient), direct, partial, stream);
         if (s != AM_OK) return s;
     }
     if (b.dw) {
@@ -272,7 +295,9 @@ am_status backward(const am_linear_config &c, const am_linear_buffers &b, const 
         a.m = (uint32_t)c.out; a.n = (uint32_t)c.in; a.k = (uint32_t)c.rows;
         a.out_f32 = sizeof(O) == 4;
         a.lda = lddz; a.ldb = (uint32_t)or_dense(c.x_stride, c.in); a.ldc = a.ldadd = (uint32_t)c.in;
-        const am_status s = launch_product<T, true, true>(a, plan_product(c, kWeightGradient), partial, stream);
+        a.k_whole = a.k;
+        const bool direct = in_chunks<T>(a.a, c.replicas, a.lda, own_dz ? sp.dz_pitch : a.m) && in_chunks<T>(a.b, c.replicas, a.ldb, a.n);
+        const am_status s = launch_product<T, true, true>(a, plan_product(c, kWeightGradient), direct, partial, stream);
         if (s != AM_OK) return s;
     }
     return AM_OK;

@@ -10,8 +10,8 @@
 namespace am {
 
 constexpr uint32_t kNormMaxReplicas = 32;
-constexpr uint32_t kNormPointers = 320;      // replicas x tensors of a launch: the arguments stay below 4 KB
-constexpr uint32_t kNormTensors = 48;        // tensors of a launch
+constexpr uint32_t kNormPointers = 304;      // replicas x tensors of a launch: the arguments stay below 4 KB
+constexpr uint32_t kNormTensors = 64;        // tensors of a launch
 
 struct NormTable {
     void *g[kNormPointers];                  // [replica][tensor of this launch]

@@ -24,9 +24,9 @@ struct QkArgs {
     uint64_t stride[2];                          // of x from token to token
     uint32_t tokens, heads[2], dim, rotated, interleaved, rows;
     uint32_t want_gain[2];                       // backward: the gain's gradient is wanted
-    uint32_t parts;                              // backward: workgroups of a replica
+    uint32_t parts[2], block;                    // workgroups of a replica for q and for k; heads of a unit
     float eps;
-    float *partial;                              // backward: [replica][part][q, k][dim]
+    float *partial[2];                           // backward: [replica][part][dim]
 };
 
 // Where the elements of pair j of a head are: the first at place_a, the second at place_a + place_step; and the column of the table (rotated pairs only)
@@ -42,26 +42,45 @@ __device__ __forceinline__ uint32_t place_step(const QkArgs &p, uint32_t j)
     return j < p.rotated / 2u ? p.rotated / 2u : (p.dim - p.rotated) / 2u;
 }
 
-// V pairs from pair j on, of which `valid` (V = 1) or all (V = 8) exist
-template <typename T, int V>
-__device__ __forceinline__ void load_pairs(const QkArgs &p, const T *head, uint32_t j, float (&a)[V], float (&b)[V])
-{
-    const T *at = head + place_a(p, j);
-    if constexpr (V == 8) {
-        if (p.interleaved) {
-            const F8 l = load8(at, 8), h = load8(at + 8, 8);
+// V pairs from pair j on as they lie in memory, and as numbers
+template <typename T, int V> struct RawPairs {
+    static constexpr int kWords = V * (int)sizeof(T) / 16;
+    u32x4 lo[kWords], hi[kWords];            // interleaved: the pairs one after the other; else the first and the second elements
+    __device__ __forceinline__ void load(const QkArgs &p, const T *head, uint32_t j)
+    {
+        const T *at = head + place_a(p, j), *next = p.interleaved ? at + V : at + place_step(p, j);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { a[i] = l.v[2 * i]; b[i] = l.v[2 * i + 1]; a[4 + i] = h.v[2 * i]; b[4 + i] = h.v[2 * i + 1]; }
-        } else {
-            const F8 l = load8(at, 8), h = load8(at + place_step(p, j), 8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { a[i] = l.v[i]; b[i] = h.v[i]; }
-        }
-    } else {
-        a[0] = to_f32(at[0]);
-        b[0] = to_f32(at[place_step(p, j)]);
+        for (int i = 0; i < kWords; ++i) { lo[i] = load16(at + i * (16 / (int)sizeof(T))); hi[i] = load16(next + i * (16 / (int)sizeof(T))); }
     }
-}
+    static __device__ __forceinline__ float number(const u32x4 (&w)[kWords], int i)
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i / 4][i & 3]);
+        else return __uint_as_float(i & 1 ? w[i / 8][i / 2 & 3] & 0xFFFF0000u : w[i / 8][i / 2 & 3] << 16);
+    }
+    __device__ __forceinline__ void numbers(const QkArgs &p, float (&a)[V], float (&b)[V]) const
+    {
+        if (p.interleaved) {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                a[i] = number(lo, 2 * i); b[i] = number(lo, 2 * i + 1);
+                a[V / 2 + i] = number(hi, 2 * i); b[V / 2 + i] = number(hi, 2 * i + 1);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) { a[i] = number(lo, i); b[i] = number(hi, i); }
+        }
+    }
+};
+template <typename T> struct RawPairs<T, 1> {
+    T lo, hi;
+    __device__ __forceinline__ void load(const QkArgs &p, const T *head, uint32_t j)
+    {
+        const T *at = head + place_a(p, j);
+        lo = at[0];
+        hi = at[place_step(p, j)];
+    }
+    __device__ __forceinline__ void numbers(const QkArgs &, float (&a)[1], float (&b)[1]) const { a[0] = to_f32(lo); b[0] = to_f32(hi); }
+};
 
 template <typename T, int V>
 __device__ __forceinline__ void store_pairs(const QkArgs &p, T *head, uint32_t j, const float (&a)[V], const float (&b)[V])
@@ -86,165 +105,199 @@ __device__ __forceinline__ void store_pairs(const QkArgs &p, T *head, uint32_t j
     }
 }
 
+// The angles of V pairs from pair j on of a row of the tables; no branch hangs on a lane, so that nothing waits for the loads here.
 template <int V>
 __device__ __forceinline__ void load_angles(const QkArgs &p, uint32_t row, uint32_t j, float (&c)[V], float (&s)[V])
 {
     const uint32_t half = p.rotated / 2u;
-    if (j >= half) {
+    if (half == 0u) {
 #pragma unroll
         for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
-    } else if (row >= p.rows) {
+        return;
+    }
+    const bool turned = j < half, known = row < p.rows;
+    const uint64_t at = (uint64_t)(known ? row : 0u) * half + (turned ? j : 0u);
 #pragma unroll
-        for (int i = 0; i < V; ++i) c[i] = s[i] = __builtin_nanf("");
-    } else {
-        const float *pc = p.cos + (uint64_t)row * half + j, *ps = p.sin + (uint64_t)row * half + j;
-        if constexpr (V == 8) {
-            const F8 x = load8(pc, 8), y = load8(ps, 8);
+    for (int i = 0; i < V; i += 4) {
+        if constexpr (V == 1) { c[0] = p.cos[at]; s[0] = p.sin[at]; }
+        else {
+            const f32x4 x = __builtin_bit_cast(f32x4, load16(p.cos + at + i)), y = __builtin_bit_cast(f32x4, load16(p.sin + at + i));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { c[i] = x.v[i]; s[i] = y.v[i]; }
-        } else {
-            c[0] = pc[0];
-            s[0] = ps[0];
+            for (int k = 0; k < 4; ++k) { c[i + k] = x[k]; s[i + k] = y[k]; }
         }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        c[i] = turned ? (known ? c[i] : __builtin_nanf("")) : 1.f;
+        s[i] = turned ? (known ? s[i] : __builtin_nanf("")) : 0.f;
     }
 }
 
-// sum over the `lanes` (a power of two) neighbouring lanes of a head
+// x of the lane that DPP control CTRL names
+template <int CTRL> __device__ __forceinline__ float other_lane(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+
+// Sum over the `lanes` (a power of two, the same for the launch) neighbouring lanes of a head.  Up to sixteen lanes without LDS:
+// exchanges within four lanes, then mirrors of eight and sixteen, whose halves hold one value each by then.
 __device__ __forceinline__ float sum_lanes(float x, int lanes)
 {
-    for (int off = 1; off < lanes; off <<= 1) x += __shfl_xor(x, off, 64);
+    if (lanes > 1) x += other_lane<0xB1>(x);         // quad_perm [1, 0, 3, 2]
+    if (lanes > 2) x += other_lane<0x4E>(x);         // quad_perm [2, 3, 0, 1]
+    if (lanes > 4) x += other_lane<0x141>(x);        // row_half_mirror
+    if (lanes > 8) x += other_lane<0x140>(x);        // row_mirror
+    if (lanes > 16) x += __shfl_xor(x, 16, 64);
+    if (lanes > 32) x += __shfl_xor(x, 32, 64);
     return x;
 }
 
-struct QkHead { uint32_t token, which, head; };      // which: 0 = q, 1 = k
-__device__ __forceinline__ QkHead head_of(const QkArgs &p, uint64_t at)
-{
-    const uint32_t all = p.heads[0] + p.heads[1];
-    QkHead h;
-    h.token = (uint32_t)(at / all);
-    h.head = (uint32_t)(at % all);
-    h.which = h.head >= p.heads[0];
-    h.head -= h.which ? p.heads[0] : 0u;
-    return h;
-}
-
-// V pairs a lane, N times; L lanes a head.  grid = (parts, replicas); heads are dealt out in turn.
-template <typename T, int V, int N, bool BACKWARD>
+// V pairs a lane, N times; `lanes` lanes a head.  A group of that many lanes takes a token and p.block of its heads at a time, U heads'
+// loads on their way together, so that the token's angles are fetched once for all of them.
+// grid = (parts, q and k, replicas): a workgroup has one kind of head; its groups take units of (token, block of heads) in turn.
+template <typename T, int V, int N, int U, bool BACKWARD>
 __global__ void __launch_bounds__(kQkThreads)
 k_qk_norm(const QkArgs p, const int lanes)
 {
-    extern __shared__ float sums[];               // backward: [q, k][groups of the workgroup][dim]
-    const uint32_t rep = blockIdx.y, lane = threadIdx.x & (uint32_t)(lanes - 1), group = threadIdx.x / (uint32_t)lanes;
+    extern __shared__ float sums[];               // backward: [group of the workgroup][dim]
+    const uint32_t rep = blockIdx.z, w = blockIdx.y, heads = p.heads[w];
+    if (blockIdx.x >= p.parts[w]) return;
+    const uint32_t lane = threadIdx.x & (uint32_t)(lanes - 1), group = threadIdx.x / (uint32_t)lanes;
     const uint32_t groups = kQkThreads / (uint32_t)lanes, pairs = p.dim / 2u;
-    const uint64_t all = (uint64_t)p.tokens * (p.heads[0] + p.heads[1]), stride = (uint64_t)gridDim.x * groups;
+    const uint32_t blocks = (heads + p.block - 1u) / p.block;
+    const uint64_t units = (uint64_t)p.tokens * blocks, stride = (uint64_t)p.parts[w] * groups;
     const float inv = 1.f / (float)p.dim;
-    float ga[2][N][V], gb[2][N][V], da[2][N][V], db[2][N][V];
+    float ga[N][V], gb[N][V], da[N][V], db[N][V];
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
+    for (int k = 0; k < N; ++k) {
+        const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
-#pragma unroll
-            for (int i = 0; i < V; ++i) ga[w][k][i] = gb[w][k][i] = da[w][k][i] = db[w][k][i] = 0.f;
-            if (p.heads[w] && j < pairs) load_pairs<T, V>(p, static_cast<const T *>(p.gain[w][rep]), j, ga[w][k], gb[w][k]);
-        }
-    // every lane of a head's group takes part in each turn, so that the butterflies stay whole
-    for (uint64_t at = (uint64_t)blockIdx.x * groups + group; at < all; at += stride) {
-        const QkHead h = head_of(p, at);
-        const uint32_t w = h.which;
-        const uint64_t dense = ((uint64_t)h.token * p.heads[w] + h.head) * p.dim;
-        const T *x = static_cast<const T *>(p.x[w][rep]) + (uint64_t)h.token * p.stride[w] + (uint64_t)h.head * p.dim;
-        const uint32_t row = p.positions[rep] ? (uint32_t)p.positions[rep][h.token] : p.rows ? h.token % p.rows : 0u;
-        float a[N][V], b[N][V], ea[N][V], eb[N][V], c[N][V], s[N][V], square = 0.f;
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
-            if (j < pairs) {
-                load_pairs<T, V>(p, x, j, a[k], b[k]);
-                if constexpr (BACKWARD) load_pairs<T, V>(p, static_cast<const T *>(p.d[w][rep]) + dense, j, ea[k], eb[k]);
-                load_angles<V>(p, row, j, c[k], s[k]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i) a[k][i] = b[k][i] = ea[k][i] = eb[k][i] = c[k][i] = s[k][i] = 0.f;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) square += a[k][i] * a[k][i] + b[k][i] * b[k][i];
-        const float r = rsqrtf(sum_lanes(square, lanes) * inv + p.eps);
-        T *out = static_cast<T *>(p.out[w][rep]) + dense;
-        if constexpr (!BACKWARD) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
-                float oa[V], ob[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float ua = a[k][i] * r * (w ? ga[1][k][i] : ga[0][k][i]), ub = b[k][i] * r * (w ? gb[1][k][i] : gb[0][k][i]);
-                    oa[i] = ua * c[k][i] - ub * s[k][i];
-                    ob[i] = ub * c[k][i] + ua * s[k][i];
-                }
-                if (j < pairs) store_pairs<T, V>(p, out, j, oa, ob);
-            }
-        } else {
-            float dot = 0.f;
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float ua = ea[k][i] * c[k][i] + eb[k][i] * s[k][i], ub = eb[k][i] * c[k][i] - ea[k][i] * s[k][i];
-                    a[k][i] *= r;
-                    b[k][i] *= r;
-                    const float sa = ua * a[k][i], sb = ub * b[k][i];
-                    if (w) { da[1][k][i] += sa; db[1][k][i] += sb; }
-                    else { da[0][k][i] += sa; db[0][k][i] += sb; }
-                    ea[k][i] = ua * (w ? ga[1][k][i] : ga[0][k][i]);
-                    eb[k][i] = ub * (w ? gb[1][k][i] : gb[0][k][i]);
-                    dot += ea[k][i] * a[k][i] + eb[k][i] * b[k][i];
-                }
-            const float mean = sum_lanes(dot, lanes) * inv;
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
-                float oa[V], ob[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) { oa[i] = r * (ea[k][i] - a[k][i] * mean); ob[i] = r * (eb[k][i] - b[k][i] * mean); }
-                if (j < pairs) store_pairs<T, V>(p, out, j, oa, ob);
-            }
+        for (int i = 0; i < V; ++i) ga[k][i] = gb[k][i] = da[k][i] = db[k][i] = 0.f;
+        if (j < pairs) {
+            RawPairs<T, V> g;
+            g.load(p, static_cast<const T *>(p.gain[w][rep]), j);
+            g.numbers(p, ga[k], gb[k]);
         }
     }
-    if constexpr (BACKWARD) {
-        // the groups' sums, joined in their order; one of q and k after the other, so that LDS holds one
+    uint64_t unit = (uint64_t)blockIdx.x * groups + group;
+    uint32_t token = (uint32_t)(unit / blocks), block = (uint32_t)(unit - (uint64_t)token * blocks);
+    const uint32_t token_step = (uint32_t)(stride / blocks), block_step = (uint32_t)(stride - (uint64_t)token_step * blocks);
+    // every lane of a group takes part in each turn, so that its sums stay whole
+    for (; unit < units; unit += stride) {
+        const uint32_t row = p.positions[rep] ? (uint32_t)p.positions[rep][token] : p.rows ? token % p.rows : 0u;
+        float c[N][V], s[N][V];
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            if (!p.want_gain[w]) continue;            // (the same for the whole launch)
-            __syncthreads();
+        for (int k = 0; k < N; ++k) {
+            const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
+            load_angles<V>(p, row, j < pairs ? j : 0u, c[k], s[k]);
+        }
+        const uint32_t first = block * p.block, last = heads - first < p.block ? heads : first + p.block;
+        const T *x = static_cast<const T *>(p.x[w][rep]) + (uint64_t)token * p.stride[w];
+        const uint64_t dense = (uint64_t)token * heads * p.dim;
+        T *out = static_cast<T *>(p.out[w][rep]) + dense;
+        const T *d = BACKWARD ? static_cast<const T *>(p.d[w][rep]) + dense : nullptr;
+        for (uint32_t head = first; head < last; head += U) {
+            // all loads first, unconditional: heads and pairs past the end repeat others and count as zeros
+            RawPairs<T, V> rx[U][N], rd[U][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (j + i < pairs) {
-                        const uint32_t pa = place_a(p, j + i);
-                        sums[group * p.dim + pa] = da[w][k][i];
-                        sums[group * p.dim + pa + place_step(p, j + i)] = db[w][k][i];
+                for (int k = 0; k < N; ++k) {
+                    const uint32_t j = (lane + (uint32_t)(k * lanes)) * V, h = head + u < last ? head + u : last - 1u;
+                    rx[u][k].load(p, x + h * p.dim, j < pairs ? j : 0u);
+                    if constexpr (BACKWARD) rd[u][k].load(p, d + h * p.dim, j < pairs ? j : 0u);
+                }
+            float a[U][N][V], b[U][N][V], ea[U][N][V], eb[U][N][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const bool here = (lane + (uint32_t)(k * lanes)) * V < pairs && head + u < last;
+                    rx[u][k].numbers(p, a[u][k], b[u][k]);
+                    if constexpr (BACKWARD) rd[u][k].numbers(p, ea[u][k], eb[u][k]);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        a[u][k][i] = here ? a[u][k][i] : 0.f;
+                        b[u][k][i] = here ? b[u][k][i] : 0.f;
+                        if constexpr (BACKWARD) { ea[u][k][i] = here ? ea[u][k][i] : 0.f; eb[u][k][i] = here ? eb[u][k][i] : 0.f; }
                     }
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float square = 0.f;
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) square += a[u][k][i] * a[u][k][i] + b[u][k][i] * b[u][k][i];
+                const float r = rsqrtf(sum_lanes(square, lanes) * inv + p.eps);
+                float mean = 0.f;
+                if constexpr (BACKWARD) {
+                    float dot = 0.f;
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            const float ua = ea[u][k][i] * c[k][i] + eb[u][k][i] * s[k][i], ub = eb[u][k][i] * c[k][i] - ea[u][k][i] * s[k][i];
+                            a[u][k][i] *= r;
+                            b[u][k][i] *= r;
+                            da[k][i] += ua * a[u][k][i];
+                            db[k][i] += ub * b[u][k][i];
+                            ea[u][k][i] = ua * ga[k][i];
+                            eb[u][k][i] = ub * gb[k][i];
+                            dot += ea[u][k][i] * a[u][k][i] + eb[u][k][i] * b[u][k][i];
+                        }
+                    mean = sum_lanes(dot, lanes) * inv;
+                }
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
+                    float oa[V], ob[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if constexpr (BACKWARD) {
+                            oa[i] = r * (ea[u][k][i] - a[u][k][i] * mean);
+                            ob[i] = r * (eb[u][k][i] - b[u][k][i] * mean);
+                        } else {
+                            const float ua = a[u][k][i] * r * ga[k][i], ub = b[u][k][i] * r * gb[k][i];
+                            oa[i] = ua * c[k][i] - ub * s[k][i];
+                            ob[i] = ub * c[k][i] + ua * s[k][i];
+                        }
+                    }
+                    if (j < pairs && head + u < last) store_pairs<T, V>(p, out + (head + u) * p.dim, j, oa, ob);
+                }
             }
-            __syncthreads();
-            for (uint32_t e = threadIdx.x; e < p.dim; e += kQkThreads) {
-                float t = 0.f;
-                for (uint32_t g = 0; g < groups; ++g) t += sums[g * p.dim + e];
-                p.partial[(((uint64_t)rep * p.parts + blockIdx.x) * 2u + w) * p.dim + e] = t;
-            }
+        }
+        token += token_step;
+        block += block_step;
+        if (block >= blocks) { block -= blocks; ++token; }
+    }
+    if constexpr (BACKWARD) {
+        if (!p.want_gain[w]) return;              // (the same for the whole workgroup)
+        // the groups' sums, joined in their order
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const uint32_t j = (lane + (uint32_t)(k * lanes)) * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (j + i < pairs) {
+                    const uint32_t pa = place_a(p, j + i);
+                    sums[group * p.dim + pa] = da[k][i];
+                    sums[group * p.dim + pa + place_step(p, j + i)] = db[k][i];
+                }
+        }
+        __syncthreads();
+        for (uint32_t e = threadIdx.x; e < p.dim; e += kQkThreads) {
+            float t = 0.f;
+            for (uint32_t g = 0; g < groups; ++g) t += sums[g * p.dim + e];
+            p.partial[w][((uint64_t)rep * p.parts[w] + blockIdx.x) * p.dim + e] = t;
         }
     }
 }
 
 struct QkGainArgs {
     void *dgain[2][kQkMaxReplicas];
-    const float *partial;
-    uint32_t parts, dim, accumulate;
+    const float *partial[2];
+    uint32_t parts[2], dim, accumulate;
 };
 
 // grid = (elements / 16, q or k, replicas): sixteen elements by sixteen shares of the parts, joined in fp64 in a fixed order
@@ -253,12 +306,13 @@ __global__ void __launch_bounds__(256)
 k_qk_gain(const QkGainArgs p)
 {
     __shared__ double red[16][17];
-    O *out = static_cast<O *>(p.dgain[blockIdx.y][blockIdx.z]);
+    const uint32_t w = blockIdx.y;
+    O *out = static_cast<O *>(p.dgain[w][blockIdx.z]);
     if (!out) return;
     const uint32_t i = threadIdx.x & 15u, r = threadIdx.x >> 4, e = blockIdx.x * 16u + i;
     double t = 0.;
     if (e < p.dim)
-        for (uint32_t k = r; k < p.parts; k += 16u) t += (double)p.partial[(((uint64_t)blockIdx.z * p.parts + k) * 2u + blockIdx.y) * p.dim + e];
+        for (uint32_t k = r; k < p.parts[w]; k += 16u) t += (double)p.partial[w][((uint64_t)blockIdx.z * p.parts[w] + k) * p.dim + e];
     red[r][i] = t;
     __syncthreads();
     if (r == 0u && e < p.dim) {

@@ -77,39 +77,48 @@ am_status check(const am_qk_config *cfg, const am_qk_buffers *buf, bool backward
     return AM_OK;
 }
 
-// Eight pairs a lane where they lie in whole chunks, one otherwise; the lanes of a head are a power of two.
-struct Shape { int v, lanes, times; };
+// Eight pairs a lane where they lie in whole chunks, one otherwise; the lanes of a head are a power of two.  A unit has eight heads of
+// a token, fewer where that would leave compute units without one; the workgroups are as many as are resident, at most one a turn.
+struct Shape { int v, lanes, times; uint32_t block, parts[2]; };
 Shape shape_of(const am_qk_config &c)
 {
     const uint32_t pairs = c.head_dim / 2;
     Shape s;
     s.v = c.rotated / 2 % 8 == 0 && pairs % 8 == 0 ? 8 : 1;
-    const uint32_t units = pairs / (uint32_t)s.v;
+    const uint32_t each = pairs / (uint32_t)s.v;
     s.lanes = 1;
-    while (s.lanes < 64 && (uint32_t)s.lanes < units) s.lanes *= 2;
-    s.times = (int)((units + (uint32_t)s.lanes - 1) / (uint32_t)s.lanes);
-    return s;
-}
-
-// Workgroups of a replica: some 2048 in all, no more than there are turns.
-uint32_t parts_of(const am_qk_config &c, const Shape &s)
-{
-    const uint64_t groups = am::kQkThreads / (uint32_t)s.lanes, turns = (c.tokens * (c.q_heads + c.k_heads) + groups - 1) / groups;
+    while (s.lanes < 64 && (uint32_t)s.lanes < each) s.lanes *= 2;
+    s.times = (int)((each + (uint32_t)s.lanes - 1) / (uint32_t)s.lanes);
+    const uint64_t groups = am::kQkThreads / (uint32_t)s.lanes, heads = c.q_heads + c.k_heads;
+    s.block = 8;
+    while (s.block > 1 && c.replicas * c.tokens * ((heads + s.block - 1) / s.block) < groups * 1024u) s.block /= 2;
     const uint64_t most = (2048 + c.replicas - 1) / c.replicas;
-    return (uint32_t)(turns < most ? turns : most);
+    for (int w = 0; w < 2; ++w) {
+        const uint64_t mine = w ? c.k_heads : c.q_heads, units = c.tokens * ((mine + s.block - 1) / s.block);
+        const uint64_t turns = (units + groups - 1) / groups, share = (most * mine + heads - 1) / heads;
+        s.parts[w] = (uint32_t)(turns < share ? turns : share);
+    }
+    return s;
 }
 
 uint64_t space(const am_qk_config &c, const am_qk_buffers &b)
 {
     if (c.tokens == 0 || !((b.dq_gain && c.q_heads) || (b.dk_gain && c.k_heads))) return 0;
-    return 8ull * c.replicas * parts_of(c, shape_of(c)) * c.head_dim;
+    const Shape s = shape_of(c);
+    return 4ull * c.replicas * (s.parts[0] + s.parts[1]) * c.head_dim;
 }
 
-template <typename T, int V, int N, bool BACKWARD>
+float *partials(const am_qk_config &c, const am_qk_buffers &b, const Shape &s, int w)
+{
+    return static_cast<float *>(b.workspace) + (w ? (uint64_t)c.replicas * s.parts[0] * c.head_dim : 0);
+}
+
+template <typename T, int V, int N, int U, bool BACKWARD>
 void launch(const am::QkArgs &a, const am_qk_config &c, const Shape &s, hipStream_t stream)
 {
     const uint32_t lds = BACKWARD && (a.want_gain[0] || a.want_gain[1]) ? am::kQkThreads / (uint32_t)s.lanes * c.head_dim * 4u : 0u;
-    am::k_qk_norm<T, V, N, BACKWARD><<<dim3(a.parts, c.replicas), am::kQkThreads, lds, stream>>>(a, s.lanes);
+    const uint32_t most = s.parts[0] > s.parts[1] ? s.parts[0] : s.parts[1];
+    am::k_qk_norm<T, V, N, U, BACKWARD><<<dim3(most, 2, c.replicas), am::kQkThreads, lds, stream>>>(a, s.lanes);
 }
 
 template <typename T, bool BACKWARD>
@@ -129,11 +138,14 @@ am_status run(const am_qk_config &c, const am_qk_buffers &b, hipStream_t stream)
     a.tokens = (uint32_t)c.tokens; a.heads[0] = c.q_heads; a.heads[1] = c.k_heads; a.dim = c.head_dim; a.rotated = c.rotated;
     a.interleaved = c.interleaved; a.rows = (uint32_t)c.table_rows; a.eps = (float)c.eps;
     a.want_gain[0] = BACKWARD && b.dq_gain && c.q_heads; a.want_gain[1] = BACKWARD && b.dk_gain && c.k_heads;
-    a.parts = parts_of(c, s);
-    a.partial = static_cast<float *>(b.workspace);
-    if (s.v == 8) launch<T, 8, 1, BACKWARD>(a, c, s, stream);            // 32 lanes at most: 256 pairs
-    else if (s.times == 1) launch<T, 1, 1, BACKWARD>(a, c, s, stream);
-    else launch<T, 1, 4, BACKWARD>(a, c, s, stream);                    // 64 lanes, up to four pairs each
+    a.block = s.block;
+    for (int w = 0; w < 2; ++w) {
+        a.parts[w] = s.parts[w];
+        if (a.want_gain[w]) a.partial[w] = partials(c, b, s, w);
+    }
+    if (s.v == 8) launch<T, 8, 1, BACKWARD ? 2 : 4, BACKWARD>(a, c, s, stream);            // 32 lanes at most: 256 pairs
+    else if (s.times == 1) launch<T, 1, 1, 4, BACKWARD>(a, c, s, stream);
+    else launch<T, 1, 4, 2, BACKWARD>(a, c, s, stream);                                   // 64 lanes, up to four pairs each
     AM_HIP(hipGetLastError());
     return AM_OK;
 }
@@ -150,8 +162,10 @@ am_status gains(const am_qk_config &c, const am_qk_buffers &b, bool accumulate, 
     }
     if (!any) return AM_OK;
     const Shape s = shape_of(c);
-    g.partial = static_cast<const float *>(b.workspace);
-    g.parts = c.tokens ? parts_of(c, s) : 0u;
+    for (int w = 0; w < 2; ++w) {
+        g.parts[w] = c.tokens ? s.parts[w] : 0u;
+        if (g.parts[w]) g.partial[w] = partials(c, b, s, w);
+    }
     g.dim = c.head_dim; g.accumulate = accumulate;
     const dim3 grid((c.head_dim + 15u) / 16u, 2, c.replicas);
     if (c.grad_dtype == AM_F32) am::k_qk_gain<float><<<grid, 256, 0, stream>>>(g);

@@ -208,33 +208,34 @@ def linear_backward(dy, x, w, act=ACT_NONE, pre=None, dw=None, db=None, accumula
 def _norm_call(entry, grads, max_norm, out):
     grads = [list(g) for g in _replicas("grads", grads)]
     R, count = len(grads), len(grads[0])
+    out = None if out is None else _replicas("out", out, R)
     flat = [t for g in grads for t in g]
-    if len(flat) != R * count:
-        raise ValueError("grads: every replica must have the same tensors")
-    for name, tensors in (("grads", flat), ("out", [] if out is None else _replicas("out", out, R))):
-        for t in tensors:
-            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype in _DTYPES):
-                raise ValueError(f"{name} must hold contiguous float32 or bfloat16 tensors on a GPU")
-    if not flat and out is None:
+    every = flat if out is None else flat + out
+    if not every:
         raise ValueError("grads: no tensors")
-    device = flat[0].device if flat else out[0].device
-    index = device.index
-    sizes = [t.numel() for t in grads[0]]
-    types = [t.dtype for t in grads[0]]
-    for g in grads:
-        if [t.numel() for t in g] != sizes or [t.dtype for t in g] != types:
-            raise ValueError("grads: every replica must have the same tensors (number of elements and type)")
-    if any(t.get_device() != index for t in flat):
-        raise ValueError(f"grads: all tensors must be on {device}")
+    try:                                          # (hundreds of tensors: one pass in C for each question)
+        places = set(map(torch.Tensor.get_device, every))
+        dense = all(map(torch.Tensor.is_contiguous, every))
+        numel = list(map(torch.Tensor.numel, flat))
+        pointers = list(map(torch.Tensor.data_ptr, flat))
+    except TypeError:
+        raise ValueError("grads and out must hold tensors") from None
+    if len(places) != 1 or -1 in places or not dense:
+        raise ValueError("grads and out must hold contiguous tensors on one GPU")
+    types = [t.dtype for t in flat]
+    sizes, kinds = numel[:count], types[:count]
+    if numel != sizes * R or types != kinds * R:
+        raise ValueError("grads: every replica must have the same tensors (number of elements and type)")
+    device = every[0].device
+    if not set(kinds) <= _DTYPES.keys():
+        raise ValueError("grads must hold float32 or bfloat16 tensors")
     out_dtype, total = F32, sum(sizes)
     if out is not None:
-        out = list(out)
+        if out[0].dtype not in _DTYPES or any(t.numel() != total or t.dtype != out[0].dtype for t in out):
+            raise ValueError(f"out must hold {R} tensors of {total} elements, all float32 or all bfloat16")
         out_dtype = _DTYPES[out[0].dtype]
-        for t in out:
-            if t.numel() != total or t.dtype != out[0].dtype or t.device != device:
-                raise ValueError(f"out must hold {R} tensors of {total} elements and one type on {device}")
-    cfg = NormConfig(R, count, (C.c_uint64 * count)(*sizes), (C.c_uint32 * count)(*[_DTYPES[t] for t in types]), out_dtype, max_norm)
-    pointers = _table(flat)
+    cfg = NormConfig(R, count, (C.c_uint64 * count)(*sizes), (C.c_uint32 * count)(*[_DTYPES[t] for t in kinds]), out_dtype, max_norm)
+    pointers = (C.c_void_p * len(flat))(*pointers)
     outs = None if out is None else _table(out)
     result = torch.empty(2, R, dtype=torch.float32, device=device)
     need = C.c_uint64(0)
