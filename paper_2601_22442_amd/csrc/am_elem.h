@@ -19,6 +19,9 @@ template <int ALIGN> struct __attribute__((packed, aligned(ALIGN))) Chunk8 { u32
 template <typename T> __device__ __forceinline__ u32x4 load16(const T *p) { return reinterpret_cast<const Chunk16<sizeof(T)> *>(p)->v; }
 template <typename T> __device__ __forceinline__ void store16(T *p, u32x4 v) { reinterpret_cast<Chunk16<sizeof(T)> *>(p)->v = v; }
 
+// the same past the caches, for what is written once and is larger than they are
+typedef u32x4 __attribute__((aligned(2))) u32x4_anywhere;
+template <typename T> __device__ __forceinline__ void stream16(T *p, u32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4_anywhere *>(p)); }
 template <typename T> __device__ __forceinline__ void store8bytes(T *p, u32x2 v) { reinterpret_cast<Chunk8<sizeof(T)> *>(p)->v = v; }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -48,15 +51,17 @@ template <typename T> __device__ __forceinline__ F8 load8(const T *p, int valid)
     return r;
 }
 
-template <typename T> __device__ __forceinline__ void store8(T *p, int valid, const F8 &x)
+template <typename T, bool STREAM = false> __device__ __forceinline__ void store8(T *p, int valid, const F8 &x)
 {
     if (valid >= 8) {
         if constexpr (sizeof(T) == 4) {
-            store16(p, __builtin_bit_cast(u32x4, f32x4{x.v[0], x.v[1], x.v[2], x.v[3]}));
-            store16(p + 4, __builtin_bit_cast(u32x4, f32x4{x.v[4], x.v[5], x.v[6], x.v[7]}));
+            const u32x4 a = __builtin_bit_cast(u32x4, f32x4{x.v[0], x.v[1], x.v[2], x.v[3]}), b = __builtin_bit_cast(u32x4, f32x4{x.v[4], x.v[5], x.v[6], x.v[7]});
+            if constexpr (STREAM) { stream16(p, a); stream16(p + 4, b); }
+            else { store16(p, a); store16(p + 4, b); }
         } else {
             const bf16x8 h = {(__bf16)x.v[0], (__bf16)x.v[1], (__bf16)x.v[2], (__bf16)x.v[3], (__bf16)x.v[4], (__bf16)x.v[5], (__bf16)x.v[6], (__bf16)x.v[7]};
-            store16(p, __builtin_bit_cast(u32x4, h));
+            if constexpr (STREAM) stream16(p, __builtin_bit_cast(u32x4, h));
+            else store16(p, __builtin_bit_cast(u32x4, h));
         }
     } else {
 #pragma unroll

@@ -22,25 +22,37 @@ constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSi
 // ---------------------------------------------------------------------------------------------
 // activations, in fp32
 // ---------------------------------------------------------------------------------------------
-// exp(-|x|)-based forms: no overflow for any finite z, and NaN stays NaN
-__device__ __forceinline__ float sigmoid_f32(float z) { return 1.0f / (1.0f + __expf(-z)); }
-__device__ __forceinline__ float gelu_tanh_inner(float z) { return 0.7978845608028654f * (z + 0.044715f * z * z * z); }
+// An epilogue has every CU's vector units to itself while the matrix units stand still, 0.45 us a tile of 256 x 256 for every
+// instruction an element takes, so these use the hardware's 2^x and reciprocal (an ulp each) and few of the rest.
+__device__ __forceinline__ float exp_f32(float x) { return __builtin_amdgcn_exp2f(1.4426950408889634f * x); }
+__device__ __forceinline__ float sigmoid_f32(float z) { return __builtin_amdgcn_rcpf(1.0f + exp_f32(-z)); }
+__device__ __forceinline__ float gelu_tanh_inner(float z) { return z * (0.7978845608028654f + 0.035677408136300125f * z * z); }
+
+// Phi(z) = 1 - h for z >= 0 and h below, h = t (a1 + t (a2 + ... a5 t^4)) e^(-z^2 / 2) / 2, t = 1 / (1 + p |z| / sqrt 2): Abramowitz and
+// Stegun, 7.1.26, good to 0.75e-7.  e: e^(-z^2 / 2)
+__device__ __forceinline__ float normal_cdf(float z, float e)
+{
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.23164188816f * fabsf(z));
+    const float h = t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f)))) * e;
+    return z >= 0.f ? 1.0f - h : h;
+}
 
 template <int ACT> __device__ __forceinline__ float act_f32(float z)
 {
     if constexpr (ACT == kActRelu) return z < 0.f ? 0.f : z;
-    if constexpr (ACT == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.7071067811865476f));
+    if constexpr (ACT == kActGelu) return z * normal_cdf(z, exp_f32(-0.5f * z * z));
     if constexpr (ACT == kActGeluTanh) return z * sigmoid_f32(2.0f * gelu_tanh_inner(z));        // (1 + tanh u) / 2 = sigmoid(2 u)
     if constexpr (ACT == kActSilu) return z * sigmoid_f32(z);
     return z;
 }
 
+// (no infinity times zero: where the factor beside z has vanished, so has the product)
 template <int ACT> __device__ __forceinline__ float act_grad_f32(float z)
 {
     if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
     if constexpr (ACT == kActGelu) {
-        const float e = __expf(-0.5f * z * z);
-        return 0.5f * (1.0f + erff(z * 0.7071067811865476f)) + (e > 0.f ? 0.3989422804014327f * z * e : 0.f);      // (no infinity times zero)
+        const float e = exp_f32(-0.5f * z * z);
+        return normal_cdf(z, e) + (e > 0.f ? 0.3989422804014327f * z * e : 0.f);
     }
     if constexpr (ACT == kActGeluTanh) {
         const float s = sigmoid_f32(2.0f * gelu_tanh_inner(z));
@@ -72,25 +84,21 @@ struct ProductArgs {
     float *partial;                            // [split][replica][m][n] when splits > 1
 };
 
-__device__ __forceinline__ void apply_act(uint32_t act, F8 &x)
+template <int ACT, int N> __device__ __forceinline__ void act_all(F8 (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[i].v[j] = act_f32<ACT>(x[i].v[j]);
+}
+
+template <int N> __device__ __forceinline__ void apply_act(uint32_t act, F8 (&x)[N])
 {
     switch (act) {               // the same for the whole launch
-    case kActRelu:
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.v[j] = act_f32<kActRelu>(x.v[j]);
-        break;
-    case kActGelu:
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.v[j] = act_f32<kActGelu>(x.v[j]);
-        break;
-    case kActGeluTanh:
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.v[j] = act_f32<kActGeluTanh>(x.v[j]);
-        break;
-    case kActSilu:
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.v[j] = act_f32<kActSilu>(x.v[j]);
-        break;
+    case kActRelu: act_all<kActRelu>(x); break;
+    case kActGelu: act_all<kActGelu>(x); break;
+    case kActGeluTanh: act_all<kActGeluTanh>(x); break;
+    case kActSilu: act_all<kActSilu>(x); break;
     default: break;
     }
 }
@@ -101,20 +109,50 @@ __device__ __forceinline__ void add8(F8 &x, const F8 &y)
     for (int j = 0; j < 8; ++j) x.v[j] += y.v[j];
 }
 
-// bias, activation, addition and rounding of eight neighbouring n of row m; `valid` of them are inside
-template <typename T>
-__device__ __forceinline__ void finish8(const ProductArgs &p, uint32_t rep, uint32_t m, uint32_t n, int valid, const F8 &bias, F8 x)
+// Where a replica's results go
+struct Finish {
+    char *c, *pre;
+    const char *add;
+    uint32_t ldc, ldpre, ldadd, act, out_f32;
+    __device__ __forceinline__ Finish(const ProductArgs &p, uint32_t rep)
+        : c(static_cast<char *>(p.c[rep])), pre(static_cast<char *>(p.pre[rep])), add(static_cast<const char *>(p.add[rep])), ldc(p.ldc), ldpre(p.ldpre),
+          ldadd(p.ldadd), act(p.act), out_f32(p.out_f32)
+    {
+    }
+};
+
+// Bias, activation, addition and rounding of eight neighbouring n of each of N rows m.  INSIDE: all of them are inside; else `valid`
+// of the eight are, and rows from p_m on are not.
+template <typename T, int N, bool INSIDE, bool STREAM>
+__device__ __forceinline__ void finish8(const Finish &f, const uint32_t (&m)[N], uint32_t p_m, uint32_t n, int valid, const F8 &bias, F8 (&x)[N])
 {
-    add8(x, bias);
-    if (p.pre[rep]) store8(static_cast<T *>(p.pre[rep]) + (uint64_t)m * p.ldpre + n, valid, x);
-    apply_act(p.act, x);
-    const uint64_t at = (uint64_t)m * p.ldc + n, from = (uint64_t)m * p.ldadd + n;
-    if (sizeof(T) == 2 && p.out_f32) {
-        if (p.add[rep]) add8(x, load8(static_cast<const float *>(p.add[rep]) + from, valid));
-        store8(static_cast<float *>(p.c[rep]) + at, valid, x);
+    const int v = INSIDE ? 8 : valid;
+#pragma unroll
+    for (int i = 0; i < N; ++i) add8(x[i], bias);
+    if (f.pre) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (INSIDE || m[i] < p_m) store8<T, STREAM>(reinterpret_cast<T *>(f.pre) + (uint64_t)m[i] * f.ldpre + n, v, x[i]);
+    }
+    apply_act(f.act, x);
+    if (sizeof(T) == 2 && f.out_f32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (!INSIDE && m[i] >= p_m) continue;
+            if (f.add) add8(x[i], load8(reinterpret_cast<const float *>(f.add) + (uint64_t)m[i] * f.ldadd + n, v));
+            store8<float, STREAM>(reinterpret_cast<float *>(f.c) + (uint64_t)m[i] * f.ldc + n, v, x[i]);
+        }
     } else {
-        if (p.add[rep]) add8(x, load8(static_cast<const T *>(p.add[rep]) + from, valid));
-        store8(static_cast<T *>(p.c[rep]) + at, valid, x);
+        if (f.add) {
+            F8 r[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) r[i] = INSIDE || m[i] < p_m ? load8(reinterpret_cast<const T *>(f.add) + (uint64_t)m[i] * f.ldadd + n, v) : F8{};
+#pragma unroll
+            for (int i = 0; i < N; ++i) add8(x[i], r[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (INSIDE || m[i] < p_m) store8<T, STREAM>(reinterpret_cast<T *>(f.c) + (uint64_t)m[i] * f.ldc + n, v, x[i]);
     }
 }
 
@@ -150,6 +188,7 @@ static __device__ const u32x4 zero_chunk = {0u, 0u, 0u, 0u};
 template <typename T, int R, int NT, bool ACROSS, int S>
 struct Operand {
     static constexpr int kStep = S * kChunk<T>;              // k of a step
+    static constexpr bool kAcross = ACROSS;
     static constexpr int kPerThread = R * S / NT;
     static constexpr int kRowChunks = R / kChunk<T>;
     static constexpr int kBytes = R * S * 16;
@@ -178,7 +217,7 @@ struct Operand {
     static __device__ __forceinline__ int turned(int r, int c) { return S == 8 ? c ^ (r & 7) : c ^ (r >> 1 & 3); }      // eight rows, 128 bytes of banks
     static __device__ __forceinline__ int swizzle(int k, int c)
     {
-        if constexpr (sizeof(T) == 2) return c ^ ((k & 3) << 1);                 // a turned read takes two chunks of four neighbouring k
+        if constexpr (sizeof(T) == 2) return c ^ (((k & 3) << 1 | (k >> 3 & 1) << 3) & (kRowChunks - 1));      // half a wave's turned read takes two chunks of each of eight k
         else return c ^ (((k >> 2) & (kRowChunks >= 16 ? 3 : 1)) << 2);          // an element read takes four chunks of k, k + 4, k + 8, k + 12
     }
     // this thread's chunks of the step at k0; k_left elements of k exist from there on
@@ -203,12 +242,12 @@ struct Operand {
     {
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
-            const int q = (wave * kPerThread + i) * 64 + lane;
+            const uint32_t q = (uint32_t)((wave * kPerThread + i) * 64 + lane);
             if constexpr (ACROSS) {
-                const int k = q / kRowChunks, r = swizzle(k, q % kRowChunks) * kChunk<T>, last = (rows_left - 1) / kChunk<T> * kChunk<T>;
+                const int k = (int)(q / kRowChunks), r = swizzle(k, (int)(q % kRowChunks)) * kChunk<T>, last = (rows_left - 1) / kChunk<T> * kChunk<T>;
                 offset[i] = (uint32_t)(k * (uint32_t)ld + (r < last ? r : last)) * (uint32_t)sizeof(T);
             } else {
-                const int r = q / S, c = turned(r, q % S);
+                const int r = (int)(q / S), c = turned(r, (int)(q % S));
                 offset[i] = (uint32_t)((r < rows_left ? r : rows_left - 1) * (uint32_t)ld + c * kChunk<T>) * (uint32_t)sizeof(T);
             }
         }
@@ -221,8 +260,8 @@ struct Operand {
         for (int i = 0; i < kPerThread; ++i) {
             const char *at = from + offset[i];
             if (k_left < kStep) {                 // (the last step alone)
-                const int q = (wave * kPerThread + i) * 64 + lane;
-                const int k = ACROSS ? q / kRowChunks : turned(q / S, q % S) * kChunk<T>;
+                const uint32_t q = (uint32_t)((wave * kPerThread + i) * 64 + lane);
+                const int k = ACROSS ? (int)(q / kRowChunks) : turned((int)(q / S), (int)(q % S)) * kChunk<T>;
                 at = k < k_left ? at : reinterpret_cast<const char *>(&zero_chunk);
             }
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)at, (__attribute__((address_space(3))) void *)(to + i * 1024), 16, 0, 0);
@@ -233,27 +272,28 @@ struct Operand {
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) *reinterpret_cast<u32x4 *>(lds + place(i * NT + tid)) = reg[i];
     }
-    // What lane `lane` gives the matrix instruction for rows row .. row + 15 in half h of the step: for row + lane % 16 the
-    // chunk of k number 4 h + lane / 16.
-    static __device__ __forceinline__ u32x4 fragment(const char *lds, int row, int h, int lane)
+    // What lane `lane` gives the matrix instruction for rows first + 16 j .. first + 16 j + 15 in half h of the step (first: a multiple of 32):
+    // for row lane % 16 of them the chunk of k number 4 h + lane / 16.  Written so that j and h are constants added to one address.
+    static __device__ __forceinline__ u32x4 fragment(const char *lds, int first, int j, int h, int lane)
     {
-        const int i = lane & 15, g = lane >> 4;
+        const uint32_t i = lane & 15u, g = (uint32_t)lane >> 4;
         if constexpr (!ACROSS) {
-            return *reinterpret_cast<const u32x4 *>(lds + place((row + i) * S + h * 4 + g));
+            const uint32_t at = (first + i) * (S * 16u) + (uint32_t)turned((int)i, (int)g) * 16u;
+            return *reinterpret_cast<const u32x4 *>(lds + (S == 8 ? at ^ (uint32_t)(h * 64) : at) + j * (16 * S * 16));
         } else if constexpr (sizeof(T) == 2) {
             // lane i of sixteen reads four rows of k + i / 4 and gets four k of row i
             typedef __attribute__((address_space(3))) bf16x4 *lds_ptr;
-            const int c = row / 8 + ((i >> 1) & 1), k = h * 32 + g * 8 + (i >> 2);
-            const char *at = lds + (i & 1) * 8;
-            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(at + (k * kRowChunks + swizzle(k, c)) * 16));
-            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(at + ((k + 4) * kRowChunks + swizzle(k + 4, c)) * 16));
+            const uint32_t k = g * 8u + (i >> 2), c = (uint32_t)swizzle((int)k, (int)(first / 8u + (i >> 1 & 1u)));      // (32 more k swizzle alike, and so do four)
+            const char *from = lds + ((k * kRowChunks + c) * 16u ^ (uint32_t)(j * 32)) + (i & 1u) * 8u + h * (32 * kRowChunks * 16);
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)from);
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_ptr)(from + 4 * kRowChunks * 16));
             const u32x2 l = __builtin_bit_cast(u32x2, lo), u = __builtin_bit_cast(u32x2, hi);
             return u32x4{l[0], l[1], u[0], u[1]};
         } else {
-            const int k = h * 16 + g * 4, r = row + i;
+            const int k = h * 16 + (int)g * 4, r = first + j * 16 + (int)i;
             u32x4 f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<const uint32_t *>(lds + ((k + j) * kRowChunks + swizzle(k + j, r / 4)) * 16 + (r & 3) * 4);
+            for (int e = 0; e < 4; ++e) f[e] = *reinterpret_cast<const uint32_t *>(lds + ((k + e) * kRowChunks + swizzle(k + e, r / 4)) * 16 + (r & 3) * 4);
             return f;
         }
     }
@@ -290,18 +330,49 @@ __device__ __forceinline__ Where where(const ProductArgs &p, uint32_t block, uin
     return w;
 }
 
-// The wave's sums (rows wm of the tile at m0, columns wn of that at n0) through its own part of LDS, at most 64 rows at a time, kept
-// [row][n] with chunks of four n moved by the row, then the epilogue.
-template <typename T, int ROWS, int COLS>
+// Rows of a wave's sums out of its part of LDS ([row][COLS], chunks of four n moved by the row), a turn of the wave after the other, U turns at once
+template <typename T, int ROWS, int COLS, int U, bool INSIDE, bool STREAM>
+__device__ __forceinline__ void finish_rows(const ProductArgs &p, const Finish &f, const char *mine, float *part_of, uint32_t m_first, uint32_t n, int valid, const F8 &bias, int lane)
+{
+    constexpr int kLanesARow = COLS / 8, kTurn = 64 / kLanesARow;
+    const int col = lane % kLanesARow * 8;
+#pragma unroll 1
+    for (int first = lane / kLanesARow; first < ROWS; first += U * kTurn) {
+        F8 x[U];
+        uint32_t m[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = first + u * kTurn;
+            m[u] = m_first + (uint32_t)row;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 t = *reinterpret_cast<const f32x4 *>(mine + (row * (COLS / 4) + ((col / 4 + h) ^ (row & (COLS / 4 - 1)))) * 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[u].v[h * 4 + j] = t[j];
+            }
+        }
+        if (!part_of) finish8<T, U, INSIDE, STREAM>(f, m, p.m, n, valid, bias, x);
+        else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (INSIDE || m[u] < p.m) store8(part_of + (uint64_t)m[u] * p.n + n, INSIDE ? 8 : valid, x[u]);
+        }
+    }
+}
+
+// The wave's sums (ROWS rows from m_first on, COLS columns from n_first on) through its own part of LDS, at most 64 rows at a time, and the epilogue
+// (STREAM: past the caches)
+template <typename T, int ROWS, int COLS, bool STREAM>
 __device__ __forceinline__ void finish_wave(const ProductArgs &p, const Where &w, f32x4 (&acc)[ROWS / 16][COLS / 16], char *lds, uint32_t m_first, uint32_t n_first, int wave, int lane)
 {
-    constexpr int kRows = ROWS < 64 ? ROWS : 64, kCols = COLS, kLanesARow = kCols / 8;
-    char *mine = lds + wave * (kRows * kCols * 4);
-    const int col = lane % kLanesARow * 8;
-    const uint32_t n = n_first + (uint32_t)col;
+    constexpr int kRows = ROWS < 64 ? ROWS : 64, kTurn = 64 / (COLS / 8), U = kRows / kTurn < 4 ? kRows / kTurn : 4;
+    char *mine = lds + wave * (kRows * COLS * 4);
+    const uint32_t n = n_first + (uint32_t)(lane % (COLS / 8) * 8);
     const int valid = n >= p.n ? 0 : p.n - n < 8u ? (int)(p.n - n) : 8;
-    const bool whole = p.splits <= 1u;
-    const F8 bias = whole ? bias8<T>(p, w.replica, n, valid) : F8{};
+    const bool inside = m_first + ROWS <= p.m && n_first + COLS <= p.n;
+    const F8 bias = p.splits <= 1u ? bias8<T>(p, w.replica, n, valid) : F8{};
+    const Finish f(p, w.replica);
+    float *part_of = p.splits <= 1u ? nullptr : p.partial + ((uint64_t)w.split * p.replicas + w.replica) * p.m * p.n;
 #pragma unroll
     for (int part = 0; part < ROWS / kRows; ++part) {
 #pragma unroll
@@ -309,23 +380,12 @@ __device__ __forceinline__ void finish_wave(const ProductArgs &p, const Where &w
 #pragma unroll
             for (int j = 0; j < COLS / 16; ++j) {
                 const int row = i * 16 + (lane & 15), c = j * 4 + (lane >> 4);
-                *reinterpret_cast<f32x4 *>(mine + (row * (kCols / 4) + (c ^ (row & (kCols / 4 - 1)))) * 16) = acc[part * (kRows / 16) + i][j];
+                *reinterpret_cast<f32x4 *>(mine + (row * (COLS / 4) + (c ^ (row & (COLS / 4 - 1)))) * 16) = acc[part * (kRows / 16) + i][j];
             }
         // (one wave's LDS accesses are done in order)
-#pragma unroll 1
-        for (int row = lane / kLanesARow; row < kRows; row += 64 / kLanesARow) {
-            const uint32_t m = m_first + (uint32_t)(part * kRows + row);
-            if (m >= p.m || valid == 0) continue;
-            F8 x;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x4 t = *reinterpret_cast<const f32x4 *>(mine + (row * (kCols / 4) + ((col / 4 + h) ^ (row & (kCols / 4 - 1)))) * 16);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x.v[h * 4 + j] = t[j];
-            }
-            if (whole) finish8<T>(p, w.replica, m, n, valid, bias, x);
-            else store8(p.partial + (((uint64_t)w.split * p.replicas + w.replica) * p.m + m) * p.n + n, valid, x);
-        }
+        const uint32_t m = m_first + (uint32_t)(part * kRows);
+        if (inside) finish_rows<T, kRows, COLS, U, true, STREAM>(p, f, mine, part_of, m, n, valid, bias, lane);
+        else if (valid) finish_rows<T, kRows, COLS, 1, false, STREAM>(p, f, mine, part_of, m, n, valid, bias, lane);
     }
 }
 
@@ -337,9 +397,9 @@ __device__ __forceinline__ void products(const char *__restrict__ cur, f32x4 (&a
     for (int h = 0; h < 2; ++h) {
         u32x4 fa[MF], fb[NF];
 #pragma unroll
-        for (int j = 0; j < NF; ++j) fb[j] = B::fragment(cur + A::kBytes, wn + j * 16, h, lane);
+        for (int j = 0; j < NF; ++j) fb[j] = B::fragment(cur + A::kBytes, wn, j, h, lane);
 #pragma unroll
-        for (int i = 0; i < MF; ++i) fa[i] = A::fragment(cur, wm + i * 16, h, lane);
+        for (int i = 0; i < MF; ++i) fa[i] = A::fragment(cur, wm, i, h, lane);
 #pragma unroll
         for (int i = 0; i < MF; ++i)
 #pragma unroll
@@ -431,40 +491,68 @@ k_product(const ProductArgs p)
 
     __syncthreads();
     static_assert(BM / WM * (BN / WN) * 4 * NT / 64 / (BM / WM > 64 ? BM / WM / 64 : 1) <= 2 * kStage, "the sums fit");
-    finish_wave<T, BM / WM, BN / WN>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
+    finish_wave<T, BM / WM, BN / WN, false>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
 }
 
-// The 256 x 256 tile of bf16, eight waves of 128 x 64 each, two to a SIMD: while one of the two multiplies, the other reads its
-// next fragments from LDS and sets out loads.  Steps of 64 bytes of k in four stages of LDS.  The waves of the second group of
-// four run half a step behind: between two barriers group 0 does memory for step q (interval 2q), then products (2q + 1); group 1
-// memory in 2q + 1, products in 2q + 2.  What the barriers then promise:
-//   step q is read in intervals 2q and 2q + 1, and the reads are over by the end of 2q + 2 (a wave's products wait for them);
-//   group 0 sets out step q + 2 in interval 2q, over step q - 2, read until 2q - 2; group 1 sets out its share of step q + 3 in
-//   2q + 1, over step q - 1, read until 2q;
-//   step q + 1 must be there before interval 2q + 2: group 0 waits for its share at the end of 2q + 1, when steps q + 1 and q + 2
-//   are on their way, group 1 at the end of 2q + 1 too, with q + 1, q + 2 and q + 3 on their way.
-// Steps past the end set out zeros, so that the counts stay.
-__device__ __forceinline__ void meet()
-{
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
+// The 256 x 256 tile of bf16: eight waves of 128 x 64, two to a SIMD.  Steps of 128 bytes of k (whole
+// lines of memory) in two halves of LDS.  A wave's stream never stops for LDS: while it multiplies the fragments of one half step it
+// reads those of the next.  Step t's halves are h0, h1:
+//   products (t, h0), meanwhile read (t, h1);
+//   wait until step t + 1 has come and own reads of step t are done, barrier: nobody reads step t any more, all of step t + 1 is there;
+//   products (t, h1), meanwhile set out step t + 2 over step t and read (t + 1, h0).
+// So 64 KB are on their way at any time, for the length of a step.  Steps past the end set out zeros and are read but not multiplied.
 template <int COUNT> __device__ __forceinline__ void wait_loads()      // until at most COUNT vector memory accesses of the wave are on their way
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
 }
+__device__ __forceinline__ void meet()                                  // all waves' LDS reads and direct loads before here are done for all
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
-template <typename A, typename B, int MF, int NF>
-__device__ __forceinline__ void large_fetch(const char *__restrict__ cur, char *__restrict__ ahead, const A &a, const B &b, const uint32_t (&oa)[A::kPerThread],
-                                            const uint32_t (&ob)[B::kPerThread], uint32_t k0, int ka, int kb, u32x4 (&fa)[MF], u32x4 (&fb)[NF], int wm, int wn, int wave, int lane)
+template <typename T, typename A, typename B, int MF, int NF>
+__device__ __forceinline__ void fetch_half(const char *__restrict__ from, int h, u32x4 (&fa)[MF], u32x4 (&fb)[NF], int wm, int wn, int lane)
 {
 #pragma unroll
-    for (int j = 0; j < NF; ++j) fb[j] = B::fragment(cur + A::kBytes, wn + j * 16, 0, lane);
+    for (int j = 0; j < NF; ++j) fb[j] = B::fragment(from + A::kBytes, wn, j, h, lane);
 #pragma unroll
-    for (int i = 0; i < MF; ++i) fa[i] = A::fragment(cur, wm + i * 16, 0, lane);
-    a.direct(ahead, oa, k0, ka, wave, lane);
-    b.direct(ahead + A::kBytes, ob, k0, kb, wave, lane);
+    for (int i = 0; i < MF; ++i) fa[i] = A::fragment(from, wm, i, h, lane);
+}
+
+// The order in which a half step's 32 products, its LDS reads (two for a turned fragment) and, in the second half, 8 direct loads are
+// issued: four products at a time with reads and a load between them, so that each finds the matrix unit busy; the last eight
+// products cover the last reads' way.
+template <int READS, bool LOADS, int G = 0>
+__device__ __forceinline__ void interleave()
+{
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    if constexpr (LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+    if constexpr (G < 6) __builtin_amdgcn_sched_group_barrier(0x100, READS * (G + 1) / 6 - READS * G / 6, 0);
+    if constexpr (G < 7) interleave<READS, LOADS, G + 1>();
+}
+
+template <typename T, int MF, int NF>
+__device__ __forceinline__ void multiply_half(const u32x4 (&fa)[MF], const u32x4 (&fb)[NF], f32x4 (&acc)[MF][NF])
+{
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+}
+
+// `over` is written by direct loads while `from` is read
+template <typename T, typename A, typename B, int MF, int NF>
+__device__ __forceinline__ void second_half(const char *__restrict__ from, char *__restrict__ over, const A &a, const B &b, const uint32_t (&oa)[A::kPerThread],
+                                            const uint32_t (&ob)[B::kPerThread], uint32_t k0, int ka, int kb, const u32x4 (&fa)[MF], const u32x4 (&fb)[NF],
+                                            u32x4 (&na)[MF], u32x4 (&nb)[NF], f32x4 (&acc)[MF][NF], int wm, int wn, int wave, int lane)
+{
+    a.direct(over, oa, k0, ka, wave, lane);
+    b.direct(over + A::kBytes, ob, k0, kb, wave, lane);
+    fetch_half<T, A, B, MF, NF>(from, 0, na, nb, wm, wn, lane);
+    multiply_half<T, MF, NF>(fa, fb, acc);
+    interleave<MF * (A::kAcross ? 2 : 1) + NF * (B::kAcross ? 2 : 1), true>();
 }
 
 template <bool A_ACROSS, bool B_ACROSS>
@@ -473,12 +561,12 @@ k_product_large(const ProductArgs p)
 {
     typedef __bf16 T;
     constexpr int BM = 256, BN = 256, NT = 512, MF = 8, NF = 4;
-    using A = Operand<T, BM, NT, A_ACROSS, 4>;
-    using B = Operand<T, BN, NT, B_ACROSS, 4>;
-    constexpr int kStep = A::kStep, kStage = A::kBytes + B::kBytes, kLoads = A::kPerThread + B::kPerThread;
+    using A = Operand<T, BM, NT, A_ACROSS, 8>;
+    using B = Operand<T, BN, NT, B_ACROSS, 8>;
+    constexpr int kStep = A::kStep, kStage = A::kBytes + B::kBytes;
     extern __shared__ __align__(16) char lds[];
 
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = wave >> 2;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Where w = where(p, blockIdx.x, gridDim.x);
     const uint32_t m0 = w.tile_m * BM, n0 = w.tile_n * BN;
     const int wm = wave / 4 * 128, wn = wave % 4 * 64;
@@ -500,40 +588,30 @@ k_product_large(const ProductArgs p)
         for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     const int extra = (int)(p.k_whole - p.k), all = (int)(k_end - k_first);
-    const auto set_out = [&](int step) {
-        char *to = lds + (step & 3) * kStage;
-        const uint32_t k0 = step < steps ? k_first + (uint32_t)step * kStep : k_first;      // (past the end: no address of it is used)
-        const int left = all - step * kStep;
-        a.direct(to, oa, k0, A_ACROSS ? left : left + extra, wave, lane);
-        b.direct(to + A::kBytes, ob, k0, B_ACROSS ? left : left + extra, wave, lane);
-    };
-    set_out(0);
-    set_out(1);
-    if (group) { set_out(2); wait_loads<2 * kLoads>(); }
-    else wait_loads<kLoads>();
-    meet();
-    if (group) meet();
-    for (int q = 0; q < steps; ++q) {
-        u32x4 fa[MF], fb[NF];
-        const int s = q + 2 + group, left = all - s * kStep;
-        const uint32_t k0 = s < steps ? k_first + (uint32_t)s * kStep : k_first;
-        large_fetch<A, B, MF, NF>(lds + (q & 3) * kStage, lds + (s & 3) * kStage, a, b, oa, ob, k0, A_ACROSS ? left : left + extra, B_ACROSS ? left : left + extra,
-                                  fa, fb, wm, wn, wave, lane);
-        if (group) wait_loads<2 * kLoads>();
-        meet();
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int i = 0; i < MF; ++i)
-#pragma unroll
-            for (int j = 0; j < NF; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
-        __builtin_amdgcn_s_setprio(0);
-        if (!group) wait_loads<kLoads>();
-        meet();
+    const auto start = [&](int step) { return step < steps ? k_first + (uint32_t)step * kStep : k_first; };      // (past the end no address of it is used)
+    const auto left = [&](int step, bool across) { return all - step * kStep + (across ? 0 : extra); };
+    for (int t = 0; t < 2; ++t) {
+        a.direct(lds + t * kStage, oa, start(t), left(t, A_ACROSS), wave, lane);
+        b.direct(lds + t * kStage + A::kBytes, ob, start(t), left(t, B_ACROSS), wave, lane);
     }
-    if (!group) meet();
+    wait_loads<A::kPerThread + B::kPerThread>();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    u32x4 fa0[MF], fb0[NF], fa1[MF], fb1[NF];
+    fetch_half<T, A, B, MF, NF>(lds, 0, fa0, fb0, wm, wn, lane);
+    for (int t = 0; t < steps; ++t) {
+        char *cur = lds + (t & 1) * kStage, *next = lds + ((t + 1) & 1) * kStage;
+        fetch_half<T, A, B, MF, NF>(cur, 1, fa1, fb1, wm, wn, lane);
+        multiply_half<T, MF, NF>(fa0, fb0, acc);
+        interleave<MF * (A_ACROSS ? 2 : 1) + NF * (B_ACROSS ? 2 : 1), false>();
+        meet();
+        second_half<T, A, B, MF, NF>(next, cur, a, b, oa, ob, start(t + 2), left(t + 2, A_ACROSS), left(t + 2, B_ACROSS), fa1, fb1, fa0, fb0, acc, wm, wn, wave, lane);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     wait_loads<0>();
     __syncthreads();
-    finish_wave<T, 128, 64>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
+    finish_wave<T, 128, 64, true>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
 }
 
 // The parts of k that workgroups summed apart, joined in their order, and the epilogue.
@@ -546,9 +624,11 @@ k_product_join(const ProductArgs p)
     for (uint64_t at = (uint64_t)blockIdx.x * 256u + threadIdx.x; at < all; at += (uint64_t)gridDim.x * 256u) {
         const uint32_t m = (uint32_t)(at / groups), n = (uint32_t)(at % groups) * 8u;
         const int valid = p.n - n < 8u ? (int)(p.n - n) : 8;
-        F8 x = {};
-        for (uint32_t s = 0; s < p.splits; ++s) add8(x, load8(p.partial + (((uint64_t)s * p.replicas + rep) * p.m + m) * p.n + n, valid));
-        finish8<T>(p, rep, m, n, valid, bias8<T>(p, rep, n, valid), x);
+        F8 x[1] = {};
+#pragma unroll 4
+        for (uint32_t s = 0; s < p.splits; ++s) add8(x[0], load8(p.partial + (((uint64_t)s * p.replicas + rep) * p.m + m) * p.n + n, valid));
+        const uint32_t rows[1] = {m};
+        finish8<T, 1, false, false>(Finish(p, rep), rows, p.m, n, valid, bias8<T>(p, rep, n, valid), x);
     }
 }
 
