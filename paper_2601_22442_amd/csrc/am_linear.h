@@ -644,27 +644,37 @@ struct ColumnArgs {
     float *partial;                              // [replica][part][n]; NULL: no sums wanted
 };
 
-// A workgroup takes 256 columns of rows_per_part rows: eight rows at a time, eight columns a thread.
+// A workgroup takes 256 columns of rows_per_part rows: eight rows at a time, eight columns a thread, the loads of U turns on their way together.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 k_columns(const ColumnArgs p)
 {
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;
     __shared__ float sums[8][256];
     const uint32_t rep = blockIdx.z, tid = threadIdx.x, c = tid & 31u, r = tid >> 5;
     const uint32_t n = blockIdx.x * 256u + c * 8u;
     const int valid = p.n <= n ? 0 : (p.n - n < 8u ? (int)(p.n - n) : 8);
     const uint32_t first = blockIdx.y * p.rows_per_part, last = p.m - first < p.rows_per_part ? p.m : first + p.rows_per_part;
+    const T *dys = static_cast<const T *>(p.dy[rep]) + n, *zs = ACT == kActNone ? nullptr : static_cast<const T *>(p.pre[rep]) + n;
+    T *dzs = static_cast<T *>(p.dz[rep]);
     F8 acc = {};
-    if (valid > 0) {
-        for (uint32_t m = first + r; m < last; m += 8u) {
-            F8 d = load8(static_cast<const T *>(p.dy[rep]) + (uint64_t)m * p.lddy + n, valid);
-            if constexpr (ACT != kActNone) {
-                const F8 z = load8(static_cast<const T *>(p.pre[rep]) + (uint64_t)m * p.ldpre + n, valid);
+    for (uint32_t m = first + r; m < last && valid > 0; m += 8u * U) {
+        F8 d[U], z[U];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d.v[j] *= act_grad_f32<ACT>(z.v[j]);
+        for (int u = 0; u < U; ++u) {
+            const uint64_t row = m + 8u * u < last ? m + 8u * u : m;           // (rows past the end repeat this one and are left out below)
+            d[u] = load8(dys + row * p.lddy, valid);
+            if constexpr (ACT != kActNone) z[u] = load8(zs + row * p.ldpre, valid);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (m + 8u * u >= last) continue;
+            if constexpr (ACT != kActNone) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[u].v[j] *= act_grad_f32<ACT>(z[u].v[j]);
             }
-            if (p.dz[rep]) store8(static_cast<T *>(p.dz[rep]) + (uint64_t)m * p.lddz + n, 8, d);       // (rows are padded to eight with zeros)
-            add8(acc, d);
+            if (dzs) store8(dzs + (uint64_t)(m + 8u * u) * p.lddz + n, 8, d[u]);       // (rows are padded to eight with zeros)
+            add8(acc, d[u]);
         }
     }
     if (!p.partial) return;
@@ -679,17 +689,45 @@ k_columns(const ColumnArgs p)
     p.partial[((uint64_t)rep * p.parts + blockIdx.y) * p.n + col] = s;
 }
 
-// the parts of a column's sum in their order; no parts: zero
+// The parts of a column's sum, in fp64 and a fixed order; no parts: zero.  32 columns a workgroup, eight shares of the parts each.
 template <typename O>
 __global__ void __launch_bounds__(256)
 k_columns_join(const ColumnArgs p)
 {
-    const uint32_t rep = blockIdx.y, n = blockIdx.x * 256u + threadIdx.x;
-    if (n >= p.n) return;
+    __shared__ double red[8][32];
+    const uint32_t rep = blockIdx.y, c = threadIdx.x & 31u, r = threadIdx.x >> 5, n = blockIdx.x * 32u + c;
     double s = 0.;
-    for (uint32_t i = 0; i < p.parts; ++i) s += (double)p.partial[((uint64_t)rep * p.parts + i) * p.n + n];
+    if (n < p.n) {
+#pragma unroll 4
+        for (uint32_t i = r; i < p.parts; i += 8u) s += (double)p.partial[((uint64_t)rep * p.parts + i) * p.n + n];
+    }
+    red[r][c] = s;
+    __syncthreads();
+    if (r || n >= p.n) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += red[i][c];
     O *out = static_cast<O *>(p.db[rep]) + n;
     *out = from_f32<O>((float)(p.accumulate ? s + (double)to_f32(*out) : s));
+}
+
+struct PackArgs {
+    const void *from[kLinearMaxReplicas];
+    void *to[kLinearMaxReplicas];
+    uint32_t rows, width, ld, pitch;         // pitch: width rounded up to eight
+};
+
+// An operand's rows moved to aligned ones, zeros behind their end, so that products can read them straight into LDS.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_pack(const PackArgs p)
+{
+    const uint32_t groups = p.pitch / 8u, rep = blockIdx.y;
+    const uint64_t all = (uint64_t)groups * p.rows;
+    for (uint64_t at = (uint64_t)blockIdx.x * 256u + threadIdx.x; at < all; at += (uint64_t)gridDim.x * 256u) {
+        const uint32_t row = (uint32_t)(at / groups), c = (uint32_t)(at - (uint64_t)row * groups) * 8u;
+        const int valid = p.width - c < 8u ? (int)(p.width - c) : 8;
+        store8(static_cast<T *>(p.to[rep]) + (uint64_t)row * p.pitch + c, 8, load8(static_cast<const T *>(p.from[rep]) + (uint64_t)row * p.ld + c, valid));
+    }
 }
 
 // clears rows of one length (a gradient of no rows)

@@ -13,7 +13,6 @@ using am_host::aligned;
 using am_host::fail;
 
 constexpr uint64_t kMaxExtent = 1ull << 31;
-enum Form { kRows, kInputGradient, kWeightGradient };      // x w^T; dz w; dz^T x
 
 uint64_t or_dense(uint64_t stride, uint64_t dense) { return stride ? stride : dense; }
 
@@ -83,41 +82,101 @@ am_status check_backward(const am_linear_config *cfg, const am_linear_buffers *b
     return AM_OK;
 }
 
-// ---- workspace ------------------------------------------------------------------------------
+// ---- plans: what a call copies first, how its products are cut, and the workspace that takes ------------------------------
 uint64_t up256(uint64_t x) { return (x + 255u) & ~255ull; }
 
-ProductPlan plan_product(const am_linear_config &c, Form form)
+// An operand as it lies in memory: `rows` rows of `width` elements, ld apart.  k side by side, or k across the rows.
+struct Source {
+    const void *p[AM_MAX_REPLICAS];
+    uint64_t rows, width, ld;
+    bool in_chunks;              // can be read straight into LDS: whole aligned chunks of 16 bytes, offsets within a tile below 2^32
+    uint64_t zeros_to;           // its rows go on with zeros up to here (width: they do not)
+};
+
+uint64_t chunk_of(const am_linear_config &c) { return c.dtype == AM_BF16 ? 8u : 4u; }
+
+Source source(const am_linear_config &c, const void *const *p, uint64_t rows, uint64_t width, uint64_t stride)
+{
+    Source s;
+    s.rows = rows; s.width = s.zeros_to = width; s.ld = or_dense(stride, width);
+    s.in_chunks = s.ld % chunk_of(c) == 0 && width % chunk_of(c) == 0 && s.ld < (1ull << 22);
+    for (uint32_t i = 0; i < c.replicas; ++i) {
+        s.p[i] = p[i];
+        s.in_chunks = s.in_chunks && aligned(p[i], 16);
+    }
+    return s;
+}
+
+// The same moved to aligned rows at `to` (one replica after the other)
+uint64_t packed_bytes(const am_linear_config &c, const Source &s) { return up256((c.dtype == AM_BF16 ? 2u : 4u) * s.rows * ((s.width + 7u) & ~7ull)); }
+Source packed(const am_linear_config &c, const Source &s, char *to)
+{
+    Source t = s;
+    t.ld = t.zeros_to = (s.width + 7u) & ~7ull;
+    t.in_chunks = t.ld < (1ull << 22);
+    for (uint32_t i = 0; i < c.replicas; ++i) t.p[i] = to + packed_bytes(c, s) * i;
+    return t;
+}
+
+struct Planned {
+    ProductPlan cut;
+    bool direct, pack_a, pack_b;
+    uint64_t pack_a_bytes, pack_b_bytes, partial_bytes, total;
+};
+
+// C is m x n, summed over k.  Operands that are not in chunks are copied first where that is the faster way by the measured times.
+Planned plan_product(const am_linear_config &c, uint64_t m, uint64_t n, uint64_t k, const Source &a, const Source &b)
 {
     const bool bf16 = c.dtype == AM_BF16;
-    if (form == kRows) return am_host::product_plan(bf16, c.replicas, c.rows, c.out, c.in);
-    if (form == kInputGradient) return am_host::product_plan(bf16, c.replicas, c.rows, c.in, c.out);
-    return am_host::product_plan(bf16, c.replicas, c.out, c.in, c.rows);
+    Planned p = {};
+    double direct_us, staged_us;
+    const ProductPlan direct = am_host::product_plan(bf16, true, c.replicas, m, n, k, &direct_us);
+    p.pack_a = !a.in_chunks; p.pack_b = !b.in_chunks;
+    if (p.pack_a) direct_us += am_host::pack_us(c.replicas * packed_bytes(c, a));
+    if (p.pack_b) direct_us += am_host::pack_us(c.replicas * packed_bytes(c, b));
+    p.direct = (!p.pack_a || a.width < (1ull << 22) - 8u) && (!p.pack_b || b.width < (1ull << 22) - 8u);
+    p.cut = direct;
+    if (p.pack_a || p.pack_b) {
+        const ProductPlan staged = am_host::product_plan(bf16, false, c.replicas, m, n, k, &staged_us);
+        if (!p.direct || staged_us <= direct_us) {
+            p.direct = p.pack_a = p.pack_b = false;
+            p.cut = staged;
+        }
+    }
+    if (p.pack_a) p.pack_a_bytes = c.replicas * packed_bytes(c, a);
+    if (p.pack_b) p.pack_b_bytes = c.replicas * packed_bytes(c, b);
+    if (p.cut.splits > 1) p.partial_bytes = up256(4u * p.cut.splits * c.replicas * m * n);
+    p.total = p.pack_a_bytes + p.pack_b_bytes + p.partial_bytes;
+    return p;
 }
 
-uint64_t partial_bytes(const am_linear_config &c, Form form)
+Planned plan_forward(const am_linear_config &c, const am_linear_buffers &b)
 {
-    const ProductPlan p = plan_product(c, form);
-    if (p.splits <= 1) return 0;
-    const uint64_t elements = form == kRows ? c.rows * c.out : form == kInputGradient ? c.rows * c.in : c.out * c.in;
-    return up256(4u * p.splits * c.replicas * elements);
+    return plan_product(c, c.rows, c.out, c.in, source(c, b.x, c.rows, c.in, c.x_stride), source(c, b.w, c.out, c.in, 0));
 }
 
-// backward: dz | column sums' parts | parts of a product (dx's and dw's take turns)
-struct BackwardSpace {
-    uint64_t dz_pitch, dz_bytes, sums_bytes, partial, total;
+// backward: dz | column sums' parts | what the products need (dx's and dw's take turns)
+struct PlannedBackward {
+    Source dz;                   // dy itself, or rows of the workspace (p: offsets to be added to it)
+    bool own_dz;
+    uint64_t dz_bytes, sums_bytes, total;
     uint32_t rows_per_part, parts;
+    Planned dx, dw;
 };
-BackwardSpace backward_space(const am_linear_config &c, const am_linear_buffers &b)
+PlannedBackward plan_backward(const am_linear_config &c, const am_linear_buffers &b, char *workspace)
 {
-    BackwardSpace s = {};
-    const uint64_t size = c.dtype == AM_BF16 ? 2u : 4u;
-    s.dz_pitch = (c.out + 7u) & ~7ull;
-    if (c.act != AM_ACT_NONE && (b.dx || b.dw)) s.dz_bytes = up256(size * c.replicas * c.rows * s.dz_pitch);
-    if (b.db || s.dz_bytes) am_host::column_parts(c.replicas, c.rows, c.out, &s.rows_per_part, &s.parts);
+    PlannedBackward s = {};
+    s.dz = source(c, b.dy, c.rows, c.out, c.y_stride);
+    s.own_dz = (b.dx || b.dw) && (c.act != AM_ACT_NONE || !s.dz.in_chunks);
+    if (s.own_dz) {
+        s.dz_bytes = c.replicas * packed_bytes(c, s.dz);
+        s.dz = packed(c, s.dz, workspace);
+    }
+    if (b.db || s.own_dz) am_host::column_parts(c.replicas, c.rows, c.out, &s.rows_per_part, &s.parts);
     if (b.db) s.sums_bytes = up256(4u * c.replicas * (uint64_t)s.parts * c.out);
-    const uint64_t dx = b.dx ? partial_bytes(c, kInputGradient) : 0, dw = b.dw ? partial_bytes(c, kWeightGradient) : 0;
-    s.partial = dx > dw ? dx : dw;
-    s.total = s.dz_bytes + s.sums_bytes + s.partial;
+    if (b.dx) s.dx = plan_product(c, c.rows, c.in, c.out, s.dz, source(c, b.w, c.out, c.in, 0));
+    if (b.dw) s.dw = plan_product(c, c.out, c.in, c.rows, s.dz, source(c, b.x, c.rows, c.in, c.x_stride));
+    s.total = s.dz_bytes + s.sums_bytes + (s.dx.total > s.dw.total ? s.dx.total : s.dw.total);
     return s;
 }
 
@@ -164,51 +223,70 @@ am_status launch_shape(ProductArgs &a, const ProductPlan &p, hipStream_t stream)
     return launch_tiles<T, 128, 128, 2, 2, AA, BA, DIRECT>(a, stream);
 }
 
-// Whether an operand can be read straight into LDS: whole chunks of 16 bytes, aligned, and an offset within a tile that fits 32 bits.
-// side: the length of its rows in memory (k, or across the tile's rows).
 template <typename T>
-bool in_chunks(const void *const *p, uint32_t replicas, uint64_t ld, uint64_t side)
+am_status pack(const am_linear_config &c, const Source &from, const Source &to, hipStream_t stream)
 {
-    constexpr uint64_t chunk = 16 / sizeof(T);
-    bool ok = ld % chunk == 0 && side % chunk == 0 && ld < (1ull << 22);
-    for (uint32_t i = 0; i < replicas; ++i) ok = ok && aligned(p[i], 16);
-    return ok;
+    am::PackArgs a;
+    std::memset(&a, 0, sizeof a);
+    for (uint32_t i = 0; i < c.replicas; ++i) { a.from[i] = from.p[i]; a.to[i] = const_cast<void *>(to.p[i]); }
+    a.rows = (uint32_t)from.rows; a.width = (uint32_t)from.width; a.ld = (uint32_t)from.ld; a.pitch = (uint32_t)to.ld;
+    const uint64_t blocks = (to.ld / 8u * from.rows + 255u) / 256u, most = (8192u + c.replicas - 1u) / c.replicas;
+    am::k_pack<T><<<dim3((uint32_t)(blocks < most ? blocks : most), c.replicas), 256, 0, stream>>>(a);
+    AM_HIP(hipGetLastError());
+    return AM_OK;
 }
 
+// The product a plan describes: args holds C, its epilogue and m, n, k.  ACROSS: k runs across the operand's rows.
 template <typename T, bool AA, bool BA>
-am_status launch_product(ProductArgs &a, const ProductPlan &p, bool direct, float *partial, hipStream_t stream)
+am_status launch_product(const am_linear_config &c, ProductArgs &args, const Planned &p, Source a, Source b, char *space, hipStream_t stream)
 {
-    a.splits = p.splits;
-    a.split_k = p.split_k;
-    a.partial = partial;
-    const am_status s = direct ? launch_shape<T, AA, BA, true>(a, p, stream) : launch_shape<T, AA, BA, false>(a, p, stream);
-    if (s != AM_OK || p.splits <= 1) return s;
-    const uint64_t blocks = ((uint64_t)((a.n + 7u) / 8u) * a.m + 255u) / 256u;
-    am::k_product_join<T><<<dim3((uint32_t)(blocks < 4096u ? blocks : 4096u), 1, a.replicas), 256, 0, stream>>>(a);
+    if (p.pack_a) {
+        const Source t = packed(c, a, space);
+        const am_status s = pack<T>(c, a, t, stream);
+        if (s != AM_OK) return s;
+        a = t;
+    }
+    if (p.pack_b) {
+        const Source t = packed(c, b, space + p.pack_a_bytes);
+        const am_status s = pack<T>(c, b, t, stream);
+        if (s != AM_OK) return s;
+        b = t;
+    }
+    for (uint32_t i = 0; i < c.replicas; ++i) { args.a[i] = a.p[i]; args.b[i] = b.p[i]; }
+    args.lda = (uint32_t)a.ld; args.ldb = (uint32_t)b.ld;
+    args.replicas = c.replicas;
+    args.splits = p.cut.splits;
+    args.split_k = p.cut.split_k;
+    args.partial = reinterpret_cast<float *>(space + p.pack_a_bytes + p.pack_b_bytes);
+    // straight into LDS, an operand that holds k side by side gives whole chunks: to the end of k, or of the zeros that all of them have behind it
+    uint64_t whole = UINT64_MAX;
+    if (!AA) whole = a.zeros_to;
+    if (!BA && b.zeros_to < whole) whole = b.zeros_to;
+    args.k_whole = p.direct && whole != UINT64_MAX ? (uint32_t)whole : args.k;
+    const am_status s = p.direct ? launch_shape<T, AA, BA, true>(args, p.cut, stream) : launch_shape<T, AA, BA, false>(args, p.cut, stream);
+    if (s != AM_OK || p.cut.splits <= 1) return s;
+    const uint64_t blocks = ((uint64_t)((args.n + 7u) / 8u) * args.m + 255u) / 256u;
+    am::k_product_join<T><<<dim3((uint32_t)(blocks < 4096u ? blocks : 4096u), 1, args.replicas), 256, 0, stream>>>(args);
     AM_HIP(hipGetLastError());
     return AM_OK;
 }
 
 template <typename T>
-am_status forward(const am_linear_config &c, const am_linear_buffers &b, hipStream_t stream)
+am_status forward(const am_linear_config &c, const am_linear_buffers &b, const Planned &p, hipStream_t stream)
 {
     ProductArgs a;
     std::memset(&a, 0, sizeof a);
     for (uint32_t i = 0; i < c.replicas; ++i) {
-        a.a[i] = b.x[i];
-        a.b[i] = b.w[i];
         a.c[i] = b.y[i];
         if (b.bias) a.bias[i] = b.bias[i];
         if (b.residual) a.add[i] = b.residual[i];
         if (b.pre) a.pre[i] = b.pre[i];
     }
-    a.m = (uint32_t)c.rows; a.n = (uint32_t)c.out; a.k = (uint32_t)c.in; a.replicas = c.replicas;
+    a.m = (uint32_t)c.rows; a.n = (uint32_t)c.out; a.k = (uint32_t)c.in;
     a.act = c.act;
-    a.lda = (uint32_t)or_dense(c.x_stride, c.in); a.ldb = (uint32_t)c.in; a.ldc = (uint32_t)or_dense(c.y_stride, c.out);
+    a.ldc = (uint32_t)or_dense(c.y_stride, c.out);
     a.ldadd = (uint32_t)or_dense(c.residual_stride, c.out); a.ldpre = (uint32_t)or_dense(c.pre_stride, c.out);
-    a.k_whole = a.k;
-    const bool direct = in_chunks<T>(a.a, c.replicas, a.lda, a.k) && in_chunks<T>(a.b, c.replicas, a.ldb, a.k);
-    return launch_product<T, false, false>(a, plan_product(c, kRows), direct, static_cast<float *>(b.workspace), stream);
+    return launch_product<T, false, false>(c, a, p, source(c, b.x, c.rows, c.in, c.x_stride), source(c, b.w, c.out, c.in, 0), static_cast<char *>(b.workspace), stream);
 }
 
 template <typename T, int ACT>
@@ -244,60 +322,50 @@ am_status clear(const am_linear_config &c, void *const *p, uint64_t elements, hi
 }
 
 template <typename T, typename O>
-am_status backward(const am_linear_config &c, const am_linear_buffers &b, const BackwardSpace &sp, bool accumulate, hipStream_t stream)
+am_status backward(const am_linear_config &c, const am_linear_buffers &b, const PlannedBackward &sp, bool accumulate, hipStream_t stream)
 {
     if (c.rows == 0) {
         if (accumulate) return AM_OK;
         if (b.dw) { const am_status s = clear<O>(c, b.dw, c.out * c.in, stream); if (s != AM_OK) return s; }
         return b.db ? clear<O>(c, b.db, c.out, stream) : AM_OK;
     }
-    char *ws = static_cast<char *>(b.workspace);
-    char *dz = ws;
-    float *sums = reinterpret_cast<float *>(ws + sp.dz_bytes), *partial = reinterpret_cast<float *>(ws + sp.dz_bytes + sp.sums_bytes);
-    const bool own_dz = sp.dz_bytes != 0;
-    const uint64_t dz_one = sizeof(T) * c.rows * sp.dz_pitch;
-    if (b.db || own_dz) {
+    char *ws = static_cast<char *>(b.workspace), *space = ws + sp.dz_bytes + sp.sums_bytes;
+    if (b.db || sp.own_dz) {
         am::ColumnArgs a;
         std::memset(&a, 0, sizeof a);
         for (uint32_t i = 0; i < c.replicas; ++i) {
             a.dy[i] = b.dy[i];
             if (c.act != AM_ACT_NONE) a.pre[i] = b.pre[i];
-            if (own_dz) a.dz[i] = dz + dz_one * i;
+            if (sp.own_dz) a.dz[i] = const_cast<void *>(sp.dz.p[i]);
             if (b.db) a.db[i] = b.db[i];
         }
-        a.m = (uint32_t)c.rows; a.n = (uint32_t)c.out; a.lddz = (uint32_t)sp.dz_pitch;
+        a.m = (uint32_t)c.rows; a.n = (uint32_t)c.out; a.lddz = (uint32_t)sp.dz.ld;
         a.lddy = (uint32_t)or_dense(c.y_stride, c.out); a.ldpre = (uint32_t)or_dense(c.pre_stride, c.out);
         a.rows_per_part = sp.rows_per_part; a.parts = sp.parts; a.accumulate = accumulate;
-        a.partial = b.db ? sums : nullptr;
+        a.partial = b.db ? reinterpret_cast<float *>(ws + sp.dz_bytes) : nullptr;
         const am_status s = columns<T>(a, c, stream);
         if (s != AM_OK) return s;
         if (b.db) {
-            am::k_columns_join<O><<<dim3((a.n + 255u) / 256u, c.replicas), 256, 0, stream>>>(a);
+            am::k_columns_join<O><<<dim3((a.n + 31u) / 32u, c.replicas), 256, 0, stream>>>(a);
             AM_HIP(hipGetLastError());
         }
     }
-    const uint32_t lddz = own_dz ? (uint32_t)sp.dz_pitch : (uint32_t)or_dense(c.y_stride, c.out);
     ProductArgs a;
-    std::memset(&a, 0, sizeof a);
-    a.replicas = c.replicas;
-    for (uint32_t i = 0; i < c.replicas; ++i) a.a[i] = own_dz ? dz + dz_one * i : static_cast<const char *>(b.dy[i]);
     if (b.dx) {
-        for (uint32_t i = 0; i < c.replicas; ++i) { a.b[i] = b.w[i]; a.c[i] = b.dx[i]; }
+        std::memset(&a, 0, sizeof a);
+        for (uint32_t i = 0; i < c.replicas; ++i) a.c[i] = b.dx[i];
         a.m = (uint32_t)c.rows; a.n = (uint32_t)c.in; a.k = (uint32_t)c.out;
-        a.lda = lddz; a.ldb = (uint32_t)c.in; a.ldc = (uint32_t)or_dense(c.dx_stride, c.in);
-        a.k_whole = own_dz ? (uint32_t)sp.dz_pitch : a.k;
-        const bool direct = in_chunks<T>(a.a, c.replicas, a.lda, a.k_whole) && in_chunks<T>(a.b, c.replicas, a.ldb, a.n);
-        const am_status s = launch_product<T, false, true>(a, plan_product(c, kInputGradient), direct, partial, stream);
+        a.ldc = (uint32_t)or_dense(c.dx_stride, c.in);
+        const am_status s = launch_product<T, false, true>(c, a, sp.dx, sp.dz, source(c, b.w, c.out, c.in, 0), space, stream);
         if (s != AM_OK) return s;
     }
     if (b.dw) {
-        for (uint32_t i = 0; i < c.replicas; ++i) { a.b[i] = b.x[i]; a.c[i] = b.dw[i]; if (accumulate) a.add[i] = b.dw[i]; }
+        std::memset(&a, 0, sizeof a);
+        for (uint32_t i = 0; i < c.replicas; ++i) { a.c[i] = b.dw[i]; if (accumulate) a.add[i] = b.dw[i]; }
         a.m = (uint32_t)c.out; a.n = (uint32_t)c.in; a.k = (uint32_t)c.rows;
+        a.ldc = a.ldadd = (uint32_t)c.in;
         a.out_f32 = sizeof(O) == 4;
-        a.lda = lddz; a.ldb = (uint32_t)or_dense(c.x_stride, c.in); a.ldc = a.ldadd = (uint32_t)c.in;
-        a.k_whole = a.k;
-        const bool direct = in_chunks<T>(a.a, c.replicas, a.lda, own_dz ? sp.dz_pitch : a.m) && in_chunks<T>(a.b, c.replicas, a.ldb, a.n);
-        const am_status s = launch_product<T, true, true>(a, plan_product(c, kWeightGradient), direct, partial, stream);
+        const am_status s = launch_product<T, true, true>(c, a, sp.dw, sp.dz, source(c, b.x, c.rows, c.in, c.x_stride), space, stream);
         if (s != AM_OK) return s;
     }
     return AM_OK;
@@ -312,7 +380,7 @@ am_status am_linear_workspace(const am_linear_config *cfg, const am_linear_buffe
     if (!out_bytes) return fail(AM_EINVAL, "out_bytes is NULL");
     const am_status s = backward_call ? check_backward(cfg, buf) : check_forward(cfg, buf);
     if (s != AM_OK) return s;
-    *out_bytes = cfg->rows == 0 ? 0 : backward_call ? backward_space(*cfg, *buf).total : partial_bytes(*cfg, kRows);
+    *out_bytes = cfg->rows == 0 ? 0 : backward_call ? plan_backward(*cfg, *buf, nullptr).total : plan_forward(*cfg, *buf).total;
     return AM_OK;
 }
 
@@ -321,18 +389,19 @@ am_status am_linear(const am_linear_config *cfg, const am_linear_buffers *buf, v
     am_status s = check_forward(cfg, buf);
     if (s != AM_OK) return s;
     if (cfg->rows == 0) return AM_OK;
-    s = check_space(buf, partial_bytes(*cfg, kRows));
+    const Planned p = plan_forward(*cfg, *buf);
+    s = check_space(buf, p.total);
     if (s != AM_OK) return s;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return cfg->dtype == AM_BF16 ? forward<__bf16>(*cfg, *buf, stream) : forward<float>(*cfg, *buf, stream);
+    return cfg->dtype == AM_BF16 ? forward<__bf16>(*cfg, *buf, p, stream) : forward<float>(*cfg, *buf, p, stream);
 }
 
 am_status am_linear_backward(const am_linear_config *cfg, const am_linear_buffers *buf, int accumulate, void *hip_stream)
 {
     am_status s = check_backward(cfg, buf);
     if (s != AM_OK) return s;
-    BackwardSpace sp = {};
-    if (cfg->rows) sp = backward_space(*cfg, *buf);
+    PlannedBackward sp = {};
+    if (cfg->rows) sp = plan_backward(*cfg, *buf, static_cast<char *>(buf->workspace));
     s = check_space(buf, sp.total);
     if (s != AM_OK) return s;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

@@ -12,31 +12,52 @@ struct ProductPlan {
     uint32_t split_k;      // of k for each, a multiple of a step
 };
 
-// Time of a product by the rounds its workgroups take: a round lasts as long as its steps, `resident` workgroups a compute unit at a
-// time, and a sum that is split costs its parts' way through memory and a launch.
-inline ProductPlan product_plan(bool bf16, uint64_t replicas, uint64_t m, uint64_t n, uint64_t k)
+// The time of a product by what its workgroups take.  A workgroup's step (128 bytes of k of both operands) lasts `alone_us` by itself and
+// `share_us` for each workgroup of its compute unit where that is longer; `resident` of them run at a time; every workgroup costs `fixed_us` besides; a sum
+// that is split costs a launch and its parts' way through memory.  The constants fit 2200 timed products on an MI355X (16 to
+// 8192 rows, 128 to 8192 columns, one to eight replicas, 1 to 32 splits; bf16 and fp32, straight into LDS and through registers): what the rule
+// picks took 1.5 to 2.6 % more than the best of all on average, 20 % at worst (9 us against 7).
+struct TileCost { uint32_t tile, resident; double alone_us, share_us, fixed_us; };
+struct ProductCost { TileCost tiles[3]; uint32_t count; double join_us, join_tb_s; };
+
+inline const ProductCost &product_cost(bool bf16, bool direct)
 {
-    struct Shape { uint32_t tile, resident; double step_us, fixed_us; };
-    static const Shape shapes_bf16[] = {{256, 1, 1.25, 3.0}, {128, 2, 0.65, 2.0}, {64, 4, 0.45, 1.5}};
-    static const Shape shapes_f32[] = {{128, 2, 4.6, 2.0}, {64, 4, 2.4, 1.5}};
-    const Shape *shapes = bf16 ? shapes_bf16 : shapes_f32;
-    const int count = bf16 ? 3 : 2;
+    static const ProductCost bf16_direct = {{{256, 1, 1.285, 1.285, 6.35}, {128, 2, 0.654, 0.472, 3.33}, {64, 4, 0.43, 0.195, 2.12}}, 3, 3.09, 4.1};
+    static const ProductCost bf16_staged = {{{256, 1, 2.355, 2.355, 5.09}, {128, 2, 0.895, 0.895, 3.85}, {64, 4, 0.568, 0.262, 1.89}}, 3, 3.9, 4.8};
+    static const ProductCost f32_direct = {{{128, 2, 2.04, 2.04, 4.44}, {64, 4, 0.681, 0.59, 2.73}}, 2, 3.86, 5.4};
+    static const ProductCost f32_staged = {{{128, 2, 2.36, 2.11, 4.33}, {64, 4, 0.752, 0.616, 2.57}}, 2, 3.9, 4.8};
+    return bf16 ? (direct ? bf16_direct : bf16_staged) : (direct ? f32_direct : f32_staged);
+}
+
+// the best plan, and its time in *out_us
+inline ProductPlan product_plan(bool bf16, bool direct, uint64_t replicas, uint64_t m, uint64_t n, uint64_t k, double *out_us)
+{
+    const ProductCost &cost = product_cost(bf16, direct);
     const uint64_t step = bf16 ? 64 : 32, steps = (k + step - 1) / step;
     ProductPlan best = {64, 1, (uint32_t)(steps * step)};
     double best_us = -1.;
-    for (int i = 0; i < count; ++i) {
-        const Shape &s = shapes[i];
+    for (uint32_t i = 0; i < cost.count; ++i) {
+        const TileCost &s = cost.tiles[i];
         const uint64_t tiles = ((m + s.tile - 1) / s.tile) * ((n + s.tile - 1) / s.tile) * replicas;
-        for (uint64_t splits = 1; splits <= 32 && splits <= steps; splits = splits < 4 ? splits + 1 : splits * 2) {
+        for (uint64_t splits = 1; splits <= 32 && splits <= steps; splits = splits < 4 ? splits + 1 : splits % 3 == 0 ? splits / 3 * 4 : splits / 2 * 3) {
             const uint64_t each = (steps + splits - 1) / splits, used = (steps + each - 1) / each;
-            const uint64_t slots = (uint64_t)kComputeUnits * s.resident, rounds = (tiles * used + slots - 1) / slots;
-            double us = (double)rounds * ((double)each * s.step_us + s.fixed_us);
-            if (used > 1) us += 4. + (double)(used + 1) * 4. * (double)(replicas * m) * (double)n / 4e6;
+            const uint64_t on_a_unit = (tiles * used + kComputeUnits - 1) / kComputeUnits, rounds = on_a_unit / s.resident, rest = on_a_unit % s.resident;
+            const auto round_us = [&](uint64_t wgs) {
+                const double shared = (double)wgs * s.share_us;
+                return (double)each * (shared > s.alone_us ? shared : s.alone_us) + s.fixed_us;
+            };
+            double us = (double)rounds * round_us(s.resident) + (rest ? round_us(rest) : 0.);
+            if (used > 1) us += cost.join_us + (double)(used + 1) * 4. * (double)(replicas * m) * (double)n / (cost.join_tb_s * 1e6);
             if (best_us < 0. || us < best_us) { best_us = us; best = {s.tile, (uint32_t)used, (uint32_t)(each * step)}; }
+            if (tiles * splits > 4096) break;        // (more parts of a sum than workgroups can use)
         }
     }
+    *out_us = best_us;
     return best;
 }
+
+// Time of copying an operand to aligned rows first: a launch, and both ways at what a copy of strided rows reaches.
+inline double pack_us(uint64_t bytes) { return 3.5 + 2. * (double)bytes / 4e6; }
 
 // Rows for each workgroup of the column sums: some 2048 workgroups, 64 rows at least.
 inline void column_parts(uint64_t replicas, uint64_t m, uint64_t n, uint32_t *rows_per_part, uint32_t *parts)

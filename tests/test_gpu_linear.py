@@ -116,6 +116,14 @@ def test_larger_products(amlib, R, M, K, N):
     _forward_case(amlib, torch.bfloat16, R, M, K, N, "GELU_TANH", True, True, True, seed=4)
 
 
+@pytest.mark.parametrize("M,K,N,shift", [(700, 1500, 1300, 1), (600, 1001, 1024, 0), (1024, 1204, 640, 1), (640, 1100, 2050, 3)])
+def test_operands_that_are_moved_to_aligned_rows_first(amlib, M, K, N, shift):
+    for dtype in (torch.bfloat16, torch.float32):
+        _forward_case(amlib, dtype, 2, M, K, N, "SILU", True, False, True, shift=shift, seed=6)
+        _backward_case(amlib, dtype, dtype, 2, M, K, N, "NONE", shift=shift, seed=7)
+        _backward_case(amlib, dtype, torch.float32, 1, M, K, N, "RELU", pad=1, shift=shift, seed=8)
+
+
 def _backward_case(am, dtype, grad_dtype, R, M, K, N, act, bias=True, accumulate=False, need_dx=True, need_dw=True, pad=0, shift=0, seed=0):
     print("linear_backward", dtype, grad_dtype, R, M, K, N, act, bias, accumulate, need_dx, need_dw, pad, shift, flush=True)
     gen = torch.Generator().manual_seed(seed)
