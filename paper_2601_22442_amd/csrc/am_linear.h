@@ -69,12 +69,16 @@ template <int ACT> __device__ __forceinline__ float act_grad_f32(float z)
 // ---------------------------------------------------------------------------------------------
 // arguments
 // ---------------------------------------------------------------------------------------------
+// A replica's arrays side by side, so that one scalar load of the (cold) arguments brings them
+struct ProductArrays {
+    const void *a, *b;
+    void *c;
+    const void *bias;              // by n; NULL: none
+    const void *add;               // added after the activation, in C's type; NULL: none (may be C itself)
+    void *pre;                     // z in the operands' type; NULL: not kept
+};
+
 struct ProductArgs {
-    const void *a[kLinearMaxReplicas], *b[kLinearMaxReplicas];
-    void *c[kLinearMaxReplicas];
-    const void *bias[kLinearMaxReplicas];      // by n; all NULL: none
-    const void *add[kLinearMaxReplicas];       // added after the activation, in C's type; all NULL: none (may be C itself)
-    void *pre[kLinearMaxReplicas];             // z in the operands' type; all NULL: not kept
     uint32_t m, n, k;
     uint32_t k_whole;                          // k rounded up to whole chunks where the operand that holds it side by side has zeros there, else k
     uint32_t lda, ldb, ldc, ldadd, ldpre;      // elements from row to row as the operands lie in memory
@@ -82,6 +86,7 @@ struct ProductArgs {
     uint32_t act, out_f32;                     // activation; C and what is added are fp32 whatever the operands
     uint32_t splits, split_k;                  // workgroup s of a tile takes k in [s split_k, (s + 1) split_k); split_k is a multiple of the step
     float *partial;                            // [split][replica][m][n] when splits > 1
+    ProductArrays of[kLinearMaxReplicas];
 };
 
 template <int ACT, int N> __device__ __forceinline__ void act_all(F8 (&x)[N])
@@ -115,7 +120,7 @@ struct Finish {
     const char *add;
     uint32_t ldc, ldpre, ldadd, act, out_f32;
     __device__ __forceinline__ Finish(const ProductArgs &p, uint32_t rep)
-        : c(static_cast<char *>(p.c[rep])), pre(static_cast<char *>(p.pre[rep])), add(static_cast<const char *>(p.add[rep])), ldc(p.ldc), ldpre(p.ldpre),
+        : c(static_cast<char *>(p.of[rep].c)), pre(static_cast<char *>(p.of[rep].pre)), add(static_cast<const char *>(p.of[rep].add)), ldc(p.ldc), ldpre(p.ldpre),
           ldadd(p.ldadd), act(p.act), out_f32(p.out_f32)
     {
     }
@@ -159,7 +164,8 @@ __device__ __forceinline__ void finish8(const Finish &f, const uint32_t (&m)[N],
 template <typename T>
 __device__ __forceinline__ F8 bias8(const ProductArgs &p, uint32_t rep, uint32_t n, int valid)
 {
-    return p.bias[rep] ? load8(static_cast<const T *>(p.bias[rep]) + n, valid) : F8{};
+    const void *bias = p.of[rep].bias;
+    return bias ? load8(static_cast<const T *>(bias) + n, valid) : F8{};
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -299,15 +305,19 @@ struct Operand {
     }
 };
 
-template <typename T> __device__ __forceinline__ f32x4 multiply(u32x4 a, u32x4 b, f32x4 c)
+// All products of a half step's fragments; fp32 takes four k at a time, and no two that follow each other add to the same sum.
+template <typename T, int MF, int NF>
+__device__ __forceinline__ void multiply_half(const u32x4 (&fa)[MF], const u32x4 (&fb)[NF], f32x4 (&acc)[MF][NF])
 {
-    if constexpr (sizeof(T) == 2) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
-        return c;
-    }
+    for (int e = 0; e < (sizeof(T) == 2 ? 1 : 4); ++e)
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                if constexpr (sizeof(T) == 2) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[j]), __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
+                else acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(fb[j][e]), __uint_as_float(fa[i][e]), acc[i][j], 0, 0, 0);
+            }
 }
 
 // Which tile, replica and part of k a workgroup takes.  Workgroup b runs on XCD b mod 8: each XCD gets a contiguous stretch of the
@@ -400,10 +410,7 @@ __device__ __forceinline__ void products(const char *__restrict__ cur, f32x4 (&a
         for (int j = 0; j < NF; ++j) fb[j] = B::fragment(cur + A::kBytes, wn, j, h, lane);
 #pragma unroll
         for (int i = 0; i < MF; ++i) fa[i] = A::fragment(cur, wm, i, h, lane);
-#pragma unroll
-        for (int i = 0; i < MF; ++i)
-#pragma unroll
-            for (int j = 0; j < NF; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+        multiply_half<T, MF, NF>(fa, fb, acc);
     }
 }
 
@@ -443,8 +450,8 @@ k_product(const ProductArgs p)
 
     A a;
     B b;
-    a.init(p.a[w.replica], p.lda, m0, p.m);
-    b.init(p.b[w.replica], p.ldb, n0, p.n);
+    a.init(p.of[w.replica].a, p.lda, m0, p.m);
+    b.init(p.of[w.replica].b, p.ldb, n0, p.n);
     f32x4 acc[MF][NF];
 #pragma unroll
     for (int i = 0; i < MF; ++i)
@@ -533,15 +540,6 @@ __device__ __forceinline__ void interleave()
     if constexpr (G < 7) interleave<READS, LOADS, G + 1>();
 }
 
-template <typename T, int MF, int NF>
-__device__ __forceinline__ void multiply_half(const u32x4 (&fa)[MF], const u32x4 (&fb)[NF], f32x4 (&acc)[MF][NF])
-{
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
-}
-
 // `over` is written by direct loads while `from` is read
 template <typename T, typename A, typename B, int MF, int NF>
 __device__ __forceinline__ void second_half(const char *__restrict__ from, char *__restrict__ over, const A &a, const B &b, const uint32_t (&oa)[A::kPerThread],
@@ -576,8 +574,8 @@ k_product_large(const ProductArgs p)
 
     A a;
     B b;
-    a.init(p.a[w.replica], p.lda, m0, p.m);
-    b.init(p.b[w.replica], p.ldb, n0, p.n);
+    a.init(p.of[w.replica].a, p.lda, m0, p.m);
+    b.init(p.of[w.replica].b, p.ldb, n0, p.n);
     uint32_t oa[A::kPerThread], ob[B::kPerThread];
     a.offsets(oa, wave, lane);
     b.offsets(ob, wave, lane);
@@ -735,7 +733,7 @@ template <typename O>
 __global__ void __launch_bounds__(256)
 k_clear(const ProductArgs p, uint64_t elements)
 {
-    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < elements; i += (uint64_t)gridDim.x * 256u) static_cast<O *>(p.c[blockIdx.y])[i] = from_f32<O>(0.f);
+    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < elements; i += (uint64_t)gridDim.x * 256u) static_cast<O *>(p.of[blockIdx.y].c)[i] = from_f32<O>(0.f);
 }
 
 }  // namespace am

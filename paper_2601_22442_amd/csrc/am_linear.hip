@@ -252,7 +252,7 @@ am_status launch_product(const am_linear_config &c, ProductArgs &args, const Pla
         if (s != AM_OK) return s;
         b = t;
     }
-    for (uint32_t i = 0; i < c.replicas; ++i) { args.a[i] = a.p[i]; args.b[i] = b.p[i]; }
+    for (uint32_t i = 0; i < c.replicas; ++i) { args.of[i].a = a.p[i]; args.of[i].b = b.p[i]; }
     args.lda = (uint32_t)a.ld; args.ldb = (uint32_t)b.ld;
     args.replicas = c.replicas;
     args.splits = p.cut.splits;
@@ -277,10 +277,10 @@ am_status forward(const am_linear_config &c, const am_linear_buffers &b, const P
     ProductArgs a;
     std::memset(&a, 0, sizeof a);
     for (uint32_t i = 0; i < c.replicas; ++i) {
-        a.c[i] = b.y[i];
-        if (b.bias) a.bias[i] = b.bias[i];
-        if (b.residual) a.add[i] = b.residual[i];
-        if (b.pre) a.pre[i] = b.pre[i];
+        a.of[i].c = b.y[i];
+        if (b.bias) a.of[i].bias = b.bias[i];
+        if (b.residual) a.of[i].add = b.residual[i];
+        if (b.pre) a.of[i].pre = b.pre[i];
     }
     a.m = (uint32_t)c.rows; a.n = (uint32_t)c.out; a.k = (uint32_t)c.in;
     a.act = c.act;
@@ -314,7 +314,7 @@ am_status clear(const am_linear_config &c, void *const *p, uint64_t elements, hi
 {
     ProductArgs a;
     std::memset(&a, 0, sizeof a);
-    for (uint32_t i = 0; i < c.replicas; ++i) a.c[i] = p[i];
+    for (uint32_t i = 0; i < c.replicas; ++i) a.of[i].c = p[i];
     const uint64_t blocks = (elements + 255u) / 256u;
     am::k_clear<O><<<dim3((uint32_t)(blocks < 4096u ? blocks : 4096u), c.replicas), 256, 0, stream>>>(a, elements);
     AM_HIP(hipGetLastError());
@@ -353,7 +353,7 @@ am_status backward(const am_linear_config &c, const am_linear_buffers &b, const 
     ProductArgs a;
     if (b.dx) {
         std::memset(&a, 0, sizeof a);
-        for (uint32_t i = 0; i < c.replicas; ++i) a.c[i] = b.dx[i];
+        for (uint32_t i = 0; i < c.replicas; ++i) a.of[i].c = b.dx[i];
         a.m = (uint32_t)c.rows; a.n = (uint32_t)c.in; a.k = (uint32_t)c.out;
         a.ldc = (uint32_t)or_dense(c.dx_stride, c.in);
         const am_status s = launch_product<T, false, true>(c, a, sp.dx, sp.dz, source(c, b.w, c.out, c.in, 0), space, stream);
@@ -361,7 +361,7 @@ am_status backward(const am_linear_config &c, const am_linear_buffers &b, const 
     }
     if (b.dw) {
         std::memset(&a, 0, sizeof a);
-        for (uint32_t i = 0; i < c.replicas; ++i) { a.c[i] = b.dw[i]; if (accumulate) a.add[i] = b.dw[i]; }
+        for (uint32_t i = 0; i < c.replicas; ++i) { a.of[i].c = b.dw[i]; if (accumulate) a.of[i].add = b.dw[i]; }
         a.m = (uint32_t)c.out; a.n = (uint32_t)c.in; a.k = (uint32_t)c.rows;
         a.ldc = a.ldadd = (uint32_t)c.in;
         a.out_f32 = sizeof(O) == 4;

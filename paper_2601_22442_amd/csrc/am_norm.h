@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(kNormThreads)
 k_norm_finish(const double *__restrict__ partial, uint32_t parts, double max_norm, float *__restrict__ norm, float *__restrict__ factor)
 {
     double acc = 0.;
+#pragma unroll 8
     for (uint32_t i = threadIdx.x; i < parts; i += kNormThreads) acc += partial[(uint64_t)blockIdx.x * parts + i];
     const double n = sqrt(sum_of_workgroup(acc));
     if (threadIdx.x == 0) {

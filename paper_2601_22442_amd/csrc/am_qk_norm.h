@@ -14,12 +14,15 @@ namespace am {
 constexpr uint32_t kQkMaxReplicas = 32;
 constexpr int kQkThreads = 256;
 
+// A replica's arrays of one kind of head side by side, so that one scalar load of the (cold) arguments brings them
+struct QkArrays {
+    const void *x, *gain;
+    void *out;                                   // forward: the result; backward: dx
+    const void *d;                               // backward: the result's gradient
+    const int32_t *positions;                    // NULL: token mod rows
+};
+
 struct QkArgs {
-    const void *x[2][kQkMaxReplicas];            // q, k
-    const void *gain[2][kQkMaxReplicas];
-    void *out[2][kQkMaxReplicas];                // forward: the result; backward: dx
-    const void *d[2][kQkMaxReplicas];            // backward: the result's gradient
-    const int32_t *positions[kQkMaxReplicas];    // all NULL: token mod rows
     const float *cos, *sin;
     uint64_t stride[2];                          // of x from token to token
     uint32_t tokens, heads[2], dim, rotated, interleaved, rows;
@@ -27,7 +30,9 @@ struct QkArgs {
     uint32_t parts[2], block;                    // workgroups of a replica for q and for k; heads of a unit
     float eps;
     float *partial[2];                           // backward: [replica][part][dim]
+    QkArrays of[2][kQkMaxReplicas];              // q, k
 };
+static_assert(sizeof(QkArgs) < 4096, "kernel arguments");
 
 // Where the elements of pair j of a head are: the first at place_a, the second at place_a + place_step; and the column of the table (rotated pairs only)
 __device__ __forceinline__ uint32_t place_a(const QkArgs &p, uint32_t j)
@@ -162,6 +167,7 @@ k_qk_norm(const QkArgs p, const int lanes)
     extern __shared__ float sums[];               // backward: [group of the workgroup][dim]
     const uint32_t rep = blockIdx.z, w = blockIdx.y, heads = p.heads[w];
     if (blockIdx.x >= p.parts[w]) return;
+    const QkArrays of = p.of[w][rep];
     const uint32_t lane = threadIdx.x & (uint32_t)(lanes - 1), group = threadIdx.x / (uint32_t)lanes;
     const uint32_t groups = kQkThreads / (uint32_t)lanes, pairs = p.dim / 2u;
     const uint32_t blocks = (heads + p.block - 1u) / p.block;
@@ -175,7 +181,7 @@ k_qk_norm(const QkArgs p, const int lanes)
         for (int i = 0; i < V; ++i) ga[k][i] = gb[k][i] = da[k][i] = db[k][i] = 0.f;
         if (j < pairs) {
             RawPairs<T, V> g;
-            g.load(p, static_cast<const T *>(p.gain[w][rep]), j);
+            g.load(p, static_cast<const T *>(of.gain), j);
             g.numbers(p, ga[k], gb[k]);
         }
     }
@@ -184,7 +190,7 @@ k_qk_norm(const QkArgs p, const int lanes)
     const uint32_t token_step = (uint32_t)(stride / blocks), block_step = (uint32_t)(stride - (uint64_t)token_step * blocks);
     // every lane of a group takes part in each turn, so that its sums stay whole
     for (; unit < units; unit += stride) {
-        const uint32_t row = p.positions[rep] ? (uint32_t)p.positions[rep][token] : p.rows ? token % p.rows : 0u;
+        const uint32_t row = of.positions ? (uint32_t)of.positions[token] : p.rows ? token % p.rows : 0u;
         float c[N][V], s[N][V];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -192,10 +198,10 @@ k_qk_norm(const QkArgs p, const int lanes)
             load_angles<V>(p, row, j < pairs ? j : 0u, c[k], s[k]);
         }
         const uint32_t first = block * p.block, last = heads - first < p.block ? heads : first + p.block;
-        const T *x = static_cast<const T *>(p.x[w][rep]) + (uint64_t)token * p.stride[w];
+        const T *x = static_cast<const T *>(of.x) + (uint64_t)token * p.stride[w];
         const uint64_t dense = (uint64_t)token * heads * p.dim;
-        T *out = static_cast<T *>(p.out[w][rep]) + dense;
-        const T *d = BACKWARD ? static_cast<const T *>(p.d[w][rep]) + dense : nullptr;
+        T *out = static_cast<T *>(of.out) + dense;
+        const T *d = BACKWARD ? static_cast<const T *>(of.d) + dense : nullptr;
         for (uint32_t head = first; head < last; head += U) {
             // all loads first, unconditional: heads and pairs past the end repeat others and count as zeros
             RawPairs<T, V> rx[U][N], rd[U][N];
@@ -311,8 +317,10 @@ k_qk_gain(const QkGainArgs p)
     if (!out) return;
     const uint32_t i = threadIdx.x & 15u, r = threadIdx.x >> 4, e = blockIdx.x * 16u + i;
     double t = 0.;
-    if (e < p.dim)
+    if (e < p.dim) {
+#pragma unroll 8
         for (uint32_t k = r; k < p.parts[w]; k += 16u) t += (double)p.partial[w][((uint64_t)blockIdx.z * p.parts[w] + k) * p.dim + e];
+    }
     red[r][i] = t;
     __syncthreads();
     if (r == 0u && e < p.dim) {

@@ -127,9 +127,9 @@ am_status run(const am_qk_config &c, const am_qk_buffers &b, hipStream_t stream)
     am::QkArgs a;
     std::memset(&a, 0, sizeof a);
     for (uint32_t i = 0; i < c.replicas; ++i) {
-        if (c.q_heads) { a.x[0][i] = b.q[i]; a.gain[0][i] = b.q_gain[i]; a.out[0][i] = BACKWARD ? b.dq[i] : b.q_out[i]; if (BACKWARD) a.d[0][i] = b.dq_out[i]; }
-        if (c.k_heads) { a.x[1][i] = b.k[i]; a.gain[1][i] = b.k_gain[i]; a.out[1][i] = BACKWARD ? b.dk[i] : b.k_out[i]; if (BACKWARD) a.d[1][i] = b.dk_out[i]; }
-        if (b.positions) a.positions[i] = b.positions[i];
+        const int32_t *positions = b.positions ? b.positions[i] : nullptr;
+        if (c.q_heads) a.of[0][i] = {b.q[i], b.q_gain[i], BACKWARD ? b.dq[i] : b.q_out[i], BACKWARD ? b.dq_out[i] : nullptr, positions};
+        if (c.k_heads) a.of[1][i] = {b.k[i], b.k_gain[i], BACKWARD ? b.dk[i] : b.k_out[i], BACKWARD ? b.dk_out[i] : nullptr, positions};
     }
     const Shape s = shape_of(c);
     a.cos = b.cos; a.sin = b.sin;

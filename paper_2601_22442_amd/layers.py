@@ -7,6 +7,7 @@ Work is enqueued on the current stream; outputs and workspaces come from PyTorch
 from __future__ import annotations
 
 import ctypes as C
+from array import array
 
 import torch
 
@@ -37,7 +38,7 @@ lib.am_linear_backward.argtypes = [C.POINTER(LinearConfig), C.POINTER(LinearBuff
 
 class NormConfig(C.Structure):
     """Mirror of am_norm_config."""
-    _fields_ = [("replicas", C.c_uint32), ("tensors", C.c_uint32), ("numel", C.POINTER(C.c_uint64)), ("dtype", C.POINTER(C.c_uint32)),
+    _fields_ = [("replicas", C.c_uint32), ("tensors", C.c_uint32), ("numel", C.c_void_p), ("dtype", C.c_void_p),
                 ("out_dtype", C.c_uint32), ("max_norm", C.c_double)]
 
 
@@ -71,14 +72,18 @@ def _replicas(name, tensors, count=None):
     return tensors
 
 
+def _refuse(name, i, t, shape, dtype, device):
+    got = (tuple(t.shape), t.dtype, t.device) if isinstance(t, torch.Tensor) else type(t).__name__
+    raise ValueError(f"{name}[{i}] must be a {dtype} tensor of shape {shape} on {device}, got {got}")
+
+
 def _matching(name, tensors, shape, dtype, device, dense=False):
     """The raw pointers are all the C side sees: what could make a kernel read past an allocation is refused here.  Returns
     the row stride that all replicas share (0: rows are dense)."""
     stride = None
     for i, t in enumerate(tensors):
-        if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and tuple(t.shape) == shape):
-            raise ValueError(f"{name}[{i}] must be a {dtype} tensor of shape {shape} on {device}, got "
-                             f"{(tuple(t.shape), t.dtype, t.device) if isinstance(t, torch.Tensor) else type(t).__name__}")
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.device != device:
+            _refuse(name, i, t, shape, dtype, device)
         if t.is_contiguous():
             row = 0
         elif dense or len(shape) != 2 or (shape[1] > 1 and t.stride(1) != 1) or (shape[0] > 1 and t.stride(0) < shape[1]):
@@ -99,8 +104,14 @@ def _device_of(name, t):
     return t.device
 
 
-def _table(tensors):
-    return (C.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+def _fill(buf, R, tables):
+    """Pointer tables of R entries each for the named fields, side by side in one array that the caller keeps during the call."""
+    pointers = array("Q", [t.data_ptr() for tensors in tables.values() for t in tensors])
+    at = pointers.buffer_info()[0]
+    for name in tables:
+        setattr(buf, name, at)
+        at += 8 * R
+    return pointers
 
 
 def _workspace(nbytes, device):
@@ -109,26 +120,27 @@ def _workspace(nbytes, device):
 
 def _linear_call(cfg, tables, backward, accumulate, device):
     buf = LinearBuffers()
-    for name, table in tables.items():
-        setattr(buf, name, C.addressof(table))
-    need = C.c_uint64(0)
+    keep = _fill(buf, cfg.replicas, tables)
+    need = C.c_uint64()
+    cfg_ref, buf_ref = C.byref(cfg), C.byref(buf)
     with _on(device):
-        _check(lib.am_linear_workspace(C.byref(cfg), C.byref(buf), int(backward), C.byref(need)))
-        space = _workspace(need.value, device)
-        if space is not None:
+        _check(lib.am_linear_workspace(cfg_ref, buf_ref, backward, C.byref(need)))
+        if need.value:
+            space = _workspace(need.value, device)
             buf.workspace, buf.workspace_bytes = space.data_ptr(), need.value
         stream = torch.cuda.current_stream(device).cuda_stream
         if backward:
-            _check(lib.am_linear_backward(C.byref(cfg), C.byref(buf), int(accumulate), stream))
+            _check(lib.am_linear_backward(cfg_ref, buf_ref, accumulate, stream))
         else:
-            _check(lib.am_linear(C.byref(cfg), C.byref(buf), stream))
+            _check(lib.am_linear(cfg_ref, buf_ref, stream))
+    del keep
 
 
 def _check_product(x, w):
     x = _replicas("x", x)
     w = _replicas("w", w, len(x))
     device = _device_of("x", x[0])
-    if x[0].dim() != 2 or w[0].dim() != 2:
+    if x[0].dim() != 2 or not isinstance(w[0], torch.Tensor) or w[0].dim() != 2:
         raise ValueError("x and w must be lists of two-dimensional tensors")
     rows, width = x[0].shape
     out = w[0].shape[0]
@@ -145,24 +157,19 @@ def linear(x, w, bias=None, act=ACT_NONE, residual=None, with_pre=False):
     residual [rows, out], all bfloat16 or all float32; rows of x and residual may be a stride apart.  Returns the list of
     y, with with_pre the pair (y, pre), pre = x w^T + bias as linear_backward takes it."""
     x, w, device, dtype, rows, width, out, x_stride = _check_product(x, w)
-    R = len(x)
-    tables = {"x": _table(x), "w": _table(w)}
-    cfg = LinearConfig(replicas=R, dtype=_DTYPES[dtype], grad_dtype=_DTYPES[dtype], act=act, rows=rows, in_=width, out=out, x_stride=x_stride)
+    R, code = len(x), _DTYPES[dtype]
+    tables = {"x": x, "w": w}
+    cfg = LinearConfig(R, code, code, act, rows, width, out, x_stride)
     if bias is not None:
-        bias = _replicas("bias", bias, R)
+        tables["bias"] = bias = _replicas("bias", bias, R)
         _matching("bias", bias, (out,), dtype, device, dense=True)
-        tables["bias"] = _table(bias)
     if residual is not None:
-        residual = _replicas("residual", residual, R)
+        tables["residual"] = residual = _replicas("residual", residual, R)
         cfg.residual_stride = _matching("residual", residual, (rows, out), dtype, device)
-        tables["residual"] = _table(residual)
-    y = [torch.empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
-    tables["y"] = _table(y)
-    pre = None
+    tables["y"] = y = [torch.empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
     if with_pre:
-        pre = [torch.empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
-        tables["pre"] = _table(pre)
-    _linear_call(cfg, tables, False, False, device)
+        tables["pre"] = pre = [torch.empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
+    _linear_call(cfg, tables, 0, 0, device)
     return (y, pre) if with_pre else y
 
 
@@ -171,38 +178,37 @@ def linear_backward(dy, x, w, act=ACT_NONE, pre=None, dw=None, db=None, accumula
     and db [out] are where the gradients go (None: not wanted), float32 or x's type, usually views into the arrays that the step
     reads; accumulate adds to what is there.  Returns the list of dx (None without need_dx).  A residual's gradient is dy."""
     x, w, device, dtype, rows, width, out, x_stride = _check_product(x, w)
-    R = len(x)
+    R, code = len(x), _DTYPES[dtype]
     if not (need_dx or dw is not None or db is not None):
         raise ValueError("no gradient is wanted: need_dx is off, dw and db are None")
     dy = _replicas("dy", dy, R)
-    cfg = LinearConfig(replicas=R, dtype=_DTYPES[dtype], grad_dtype=_DTYPES[dtype], act=act, rows=rows, in_=width, out=out, x_stride=x_stride)
-    cfg.y_stride = _matching("dy", dy, (rows, out), dtype, device)
-    tables = {"dy": _table(dy), "x": _table(x), "w": _table(w)}
+    cfg = LinearConfig(R, code, code, act, rows, width, out, x_stride, _matching("dy", dy, (rows, out), dtype, device))
+    tables = {"dy": dy, "x": x, "w": w}
     if act != ACT_NONE:
         if pre is None:
             raise ValueError("the gradient of an activation needs pre")
-        pre = _replicas("pre", pre, R)
+        tables["pre"] = pre = _replicas("pre", pre, R)
         cfg.pre_stride = _matching("pre", pre, (rows, out), dtype, device)
-        tables["pre"] = _table(pre)
     grad_dtype = None
     for name, grads, shape in (("dw", dw, (out, width)), ("db", db, (out,))):
         if grads is None:
             continue
-        grads = _replicas(name, grads, R)
+        tables[name] = grads = _replicas(name, grads, R)
         if grad_dtype is None:
-            grad_dtype = grads[0].dtype
-            if grad_dtype not in (torch.float32, dtype):
-                raise ValueError(f"{name} must be float32 or {dtype}, not {grad_dtype}")
+            grad_dtype = _grad_type(name, grads[0], dtype)
+            cfg.grad_dtype = _DTYPES[grad_dtype]
         _matching(name, grads, shape, grad_dtype, device, dense=True)
-        tables[name] = _table(grads)
-    if grad_dtype is not None:
-        cfg.grad_dtype = _DTYPES[grad_dtype]
     dx = None
     if need_dx:
-        dx = [torch.empty((rows, width), dtype=dtype, device=device) for _ in range(R)]
-        tables["dx"] = _table(dx)
-    _linear_call(cfg, tables, True, accumulate, device)
+        tables["dx"] = dx = [torch.empty((rows, width), dtype=dtype, device=device) for _ in range(R)]
+    _linear_call(cfg, tables, 1, int(accumulate), device)
     return dx
+
+
+def _grad_type(name, t, dtype):
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, dtype):
+        raise ValueError(f"{name} must hold tensors of float32 or {dtype}")
+    return t.dtype
 
 
 def _norm_call(entry, grads, max_norm, out):
@@ -234,16 +240,17 @@ def _norm_call(entry, grads, max_norm, out):
         if out[0].dtype not in _DTYPES or any(t.numel() != total or t.dtype != out[0].dtype for t in out):
             raise ValueError(f"out must hold {R} tensors of {total} elements, all float32 or all bfloat16")
         out_dtype = _DTYPES[out[0].dtype]
-    cfg = NormConfig(R, count, (C.c_uint64 * count)(*sizes), (C.c_uint32 * count)(*[_DTYPES[t] for t in kinds]), out_dtype, max_norm)
-    pointers = (C.c_void_p * len(flat))(*pointers)
-    outs = None if out is None else _table(out)
+    sizes, pointers = array("Q", sizes), array("Q", pointers)
+    codes = array("I", [_DTYPES[t] for t in kinds])
+    outs = None if out is None else array("Q", [t.data_ptr() for t in out])
+    cfg = NormConfig(R, count, sizes.buffer_info()[0], codes.buffer_info()[0], out_dtype, max_norm)
     result = torch.empty(2, R, dtype=torch.float32, device=device)
-    need = C.c_uint64(0)
+    need = C.c_uint64()
     with _on(device):
         _check(lib.am_norm_workspace(C.byref(cfg), C.byref(need)))
         space = _workspace(need.value, device)
         at = result.data_ptr()
-        _check(entry(C.byref(cfg), pointers, outs, at, at + 4 * R, None if space is None else space.data_ptr(), need.value,
+        _check(entry(C.byref(cfg), pointers.buffer_info()[0], None if outs is None else outs.buffer_info()[0], at, at + 4 * R, None if space is None else space.data_ptr(), need.value,
                      torch.cuda.current_stream(device).cuda_stream))
     return result[0], result[1]
 
@@ -267,18 +274,18 @@ def rotation_table(rows, rotated, base=10000.0, device="cuda:0"):
     return angle.cos().float(), angle.sin().float()
 
 
-def _heads(name, tensors, tokens, heads, dim, dtype, device, dense=False):
+def _heads(name, tensors, shape, dtype, device, dense=False):
     """Checks [tokens, heads, dim] tensors; returns the stride from token to token that all replicas share (0: dense)."""
     stride = None
     for i, t in enumerate(tensors):
-        if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and tuple(t.shape) == (tokens, heads, dim)):
-            raise ValueError(f"{name}[{i}] must be a {dtype} tensor of shape {(tokens, heads, dim)} on {device}, got "
-                             f"{(tuple(t.shape), t.dtype, t.device) if isinstance(t, torch.Tensor) else type(t).__name__}")
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.device != device:
+            _refuse(name, i, t, tuple(shape), dtype, device)
         if t.is_contiguous():
             row = 0
-        elif dense or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (tokens > 1 and t.stride(0) < heads * dim):
-            raise ValueError(f"{name}[{i}] has strides {t.stride()}: " + ("it must be contiguous" if dense else "a token's heads must lie side by side"))
         else:
+            tokens, heads, dim = shape
+            if dense or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (tokens > 1 and t.stride(0) < heads * dim):
+                raise ValueError(f"{name}[{i}] has strides {t.stride()}: " + ("it must be contiguous" if dense else "a token's heads must lie side by side"))
             row = t.stride(0) if tokens > 1 else 0
         if stride is not None and row != stride:
             raise ValueError(f"{name}: all replicas must have the same stride")
@@ -293,31 +300,24 @@ def _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
     device, dtype = _device_of("q", q[0]), q[0].dtype
     if q[0].dim() != 3 or not isinstance(k[0], torch.Tensor) or k[0].dim() != 3:
         raise ValueError("q and k must be lists of [tokens, heads, dim] tensors")
-    tokens, q_heads, dim = q[0].shape
-    k_heads = k[0].shape[1]
-    cfg = QkConfig(replicas=R, dtype=_DTYPES[dtype], grad_dtype=_DTYPES[dtype], interleaved=int(bool(interleaved)), tokens=tokens, q_heads=q_heads,
-                   k_heads=k_heads, head_dim=dim, eps=eps)
-    cfg.q_stride = _heads("q", q, tokens, q_heads, dim, dtype, device)
-    cfg.k_stride = _heads("k", k, tokens, k_heads, dim, dtype, device)
+    q_shape = q[0].shape
+    tokens, q_heads, dim = q_shape
+    k_shape = torch.Size((tokens, k[0].shape[1], dim))
+    q_stride, k_stride = _heads("q", q, q_shape, dtype, device), _heads("k", k, k_shape, dtype, device)
     q_gain, k_gain = _replicas("q_gain", q_gain, R), _replicas("k_gain", k_gain, R)
     _matching("q_gain", q_gain, (dim,), dtype, device, dense=True)
     _matching("k_gain", k_gain, (dim,), dtype, device, dense=True)
     if not (isinstance(cos, torch.Tensor) and isinstance(sin, torch.Tensor) and cos.dim() == 2 and cos.shape == sin.shape):
         raise ValueError("cos and sin must be tensors of one shape [rows, rotated / 2]")
-    _matching("cos, sin", [cos, sin], tuple(cos.shape), torch.float32, device, dense=True)
-    cfg.table_rows, cfg.rotated = cos.shape[0], 2 * cos.shape[1]
-    buf, tables = QkBuffers(), {"q": _table(q), "k": _table(k), "q_gain": _table(q_gain), "k_gain": _table(k_gain)}
-    buf.cos, buf.sin = cos.data_ptr(), sin.data_ptr()
+    _matching("cos, sin", (cos, sin), cos.shape, torch.float32, device, dense=True)
+    cfg = QkConfig(R, _DTYPES[dtype], _DTYPES[dtype], 1 if interleaved else 0, tokens, q_heads, k_shape[1], dim, 2 * cos.shape[1], q_stride, k_stride, cos.shape[0], eps)
+    tables = {"q": q, "k": k, "q_gain": q_gain, "k_gain": k_gain}
     if positions is not None:
-        positions = _replicas("positions", positions, R)
+        tables["positions"] = positions = _replicas("positions", positions, R)
         _matching("positions", positions, (tokens,), torch.int32, device, dense=True)
-        tables["positions"] = _table(positions)
-    return cfg, buf, tables, device, dtype, tuple(q[0].shape), tuple(k[0].shape)
-
-
-def _fill(buf, tables):
-    for name, table in tables.items():
-        setattr(buf, name, C.addressof(table))
+    buf = QkBuffers()
+    buf.cos, buf.sin = cos.data_ptr(), sin.data_ptr()
+    return cfg, buf, tables, device, dtype, q_shape, k_shape
 
 
 def qk_norm(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, interleaved=False):
@@ -325,45 +325,44 @@ def qk_norm(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, interleave
     pairs rotated.  Lists of R tensors: q [tokens, q heads, dim], k [tokens, k heads, dim], a token's heads side by side (views into the product
     that made them); gains [dim]; cos and sin as rotation_table gives them (2 cos.shape[1] elements of a head are rotated: pairs
     (j, j + half), interleaved (2 j, 2 j + 1)); positions int32 [tokens] rows of the tables, None: token mod rows, and a row that the tables do not
-    have makes the token NaN.  Returns two lists of dense tensors."""
+    have makes the token's rotated elements NaN.  Returns two lists of dense tensors."""
     cfg, buf, tables, device, dtype, q_shape, k_shape = _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
-    outs = [[torch.empty(shape, dtype=dtype, device=device) for _ in range(cfg.replicas)] for shape in (q_shape, k_shape)]
-    tables["q_out"], tables["k_out"] = _table(outs[0]), _table(outs[1])
-    _fill(buf, tables)
+    R = cfg.replicas
+    tables["q_out"] = q_out = [torch.empty(q_shape, dtype=dtype, device=device) for _ in range(R)]
+    tables["k_out"] = k_out = [torch.empty(k_shape, dtype=dtype, device=device) for _ in range(R)]
+    keep = _fill(buf, R, tables)
     with _on(device):
         _check(lib.am_qk_norm(C.byref(cfg), C.byref(buf), torch.cuda.current_stream(device).cuda_stream))
-    return outs[0], outs[1]
+    del keep
+    return q_out, k_out
 
 
 def qk_norm_backward(dq, dk, q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, interleaved=False, dq_gain=None, dk_gain=None, accumulate=False):
     """The gradients of qk_norm (am_qk_norm_backward): dq and dk are those of its two results (dense).  dq_gain and dk_gain [dim] are where the
     gains' gradients go (None: not wanted), float32 or q's type; accumulate adds to what is there.  Returns the lists of the gradients of q and k."""
     cfg, buf, tables, device, dtype, q_shape, k_shape = _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
-    dq, dk = _replicas("dq", dq, cfg.replicas), _replicas("dk", dk, cfg.replicas)
-    _heads("dq", dq, *q_shape, dtype, device, dense=True)
-    _heads("dk", dk, *k_shape, dtype, device, dense=True)
-    tables["dq_out"], tables["dk_out"] = _table(dq), _table(dk)
+    R = cfg.replicas
+    tables["dq_out"], tables["dk_out"] = dq, dk = _replicas("dq", dq, R), _replicas("dk", dk, R)
+    _heads("dq", dq, q_shape, dtype, device, dense=True)
+    _heads("dk", dk, k_shape, dtype, device, dense=True)
     grad_dtype = None
     for name, grads in (("dq_gain", dq_gain), ("dk_gain", dk_gain)):
         if grads is None:
             continue
-        grads = _replicas(name, grads, cfg.replicas)
+        tables[name] = grads = _replicas(name, grads, R)
         if grad_dtype is None:
-            grad_dtype = grads[0].dtype
-            if grad_dtype not in (torch.float32, dtype):
-                raise ValueError(f"{name} must be float32 or {dtype}, not {grad_dtype}")
+            grad_dtype = _grad_type(name, grads[0], dtype)
+            cfg.grad_dtype = _DTYPES[grad_dtype]
         _matching(name, grads, (q_shape[2],), grad_dtype, device, dense=True)
-        tables[name] = _table(grads)
-    if grad_dtype is not None:
-        cfg.grad_dtype = _DTYPES[grad_dtype]
-    outs = [[torch.empty(shape, dtype=dtype, device=device) for _ in range(cfg.replicas)] for shape in (q_shape, k_shape)]
-    tables["dq"], tables["dk"] = _table(outs[0]), _table(outs[1])
-    _fill(buf, tables)
-    need = C.c_uint64(0)
+    tables["dq"] = q_grad = [torch.empty(q_shape, dtype=dtype, device=device) for _ in range(R)]
+    tables["dk"] = k_grad = [torch.empty(k_shape, dtype=dtype, device=device) for _ in range(R)]
+    keep = _fill(buf, R, tables)
+    need = C.c_uint64()
     with _on(device):
         _check(lib.am_qk_norm_workspace(C.byref(cfg), C.byref(buf), C.byref(need)))
-        space = _workspace(need.value, device)
-        if space is not None:
+        if need.value:
+            space = _workspace(need.value, device)
             buf.workspace, buf.workspace_bytes = space.data_ptr(), need.value
         _check(lib.am_qk_norm_backward(C.byref(cfg), C.byref(buf), int(accumulate), torch.cuda.current_stream(device).cuda_stream))
-    return outs[0], outs[1]
+    del keep
+    return q_grad, k_grad
