@@ -415,21 +415,34 @@ __device__ __forceinline__ void products(const char *__restrict__ cur, f32x4 (&a
 }
 
 // The next step's chunks set out for `next`, then the products of the step in `cur`.
-template <typename T, typename A, typename B, int MF, int NF>
+template <typename T, typename A, typename B, int MF, int NF, bool EARLY>
 __device__ __forceinline__ void direct_step(const char *__restrict__ cur, char *__restrict__ next, const A &a, const B &b,
                                             const uint32_t (&oa)[A::kPerThread], const uint32_t (&ob)[B::kPerThread], uint32_t k0, int ka, int kb,
-                                            bool more, f32x4 (&acc)[MF][NF], int wm, int wn, int wave, int lane)
+                                            f32x4 (&acc)[MF][NF], int wm, int wn, int wave, int lane)
 {
-    if (more) {
-        a.direct(next, oa, k0, ka, wave, lane);
-        b.direct(next + A::kBytes, ob, k0, kb, wave, lane);
-    }
+    a.direct(next, oa, k0, ka, wave, lane);
+    b.direct(next + A::kBytes, ob, k0, kb, wave, lane);
+    // With two stages of the 128 tile the loads go first: left to the compiler they went behind the products where B lies across
+    // (38 us for 32 us of 3 x 1112 x 2304 -> 1152).  Deeper stages of the small tile have time, and lose up to 10 % by it.
+    if constexpr (EARLY) __builtin_amdgcn_sched_barrier(0);
     products<T, A, B, MF, NF>(cur, acc, wm, wn, lane);
 }
 
-// BM x BN tile, WM x WN waves, each BM / WM by BN / WN.  LDS: two steps of both operands, one read while the next is on its way
-// (DIRECT: straight from memory, else through registers); one barrier a step.
-template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, bool DIRECT>
+template <int COUNT> __device__ __forceinline__ void wait_loads()      // until at most COUNT vector memory accesses of the wave are on their way
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
+}
+// a barrier that waits for no loads on their way; the wave's LDS reads are done (their values are used)
+__device__ __forceinline__ void barrier_alone()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// BM x BN tile, WM x WN waves, each BM / WM by BN / WN.  LDS holds STAGES steps of both operands, one read while the others are on their
+// way; one barrier a step.  DIRECT: straight from memory, else through registers (two stages).
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int STAGES>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
 k_product(const ProductArgs p)
 {
@@ -464,16 +477,25 @@ k_product(const ProductArgs p)
         b.offsets(ob, wave, lane);
         // k_end is that of k as it is summed; an operand that holds k side by side has zeros up to a whole chunk
         const int extra = (int)(p.k_whole - p.k);
-        int left = (int)(k_end - k_first);
-        const auto ends = [&](int l, bool across) { return across ? l : l + extra; };
-        a.direct(lds, oa, k_first, ends(left, A_ACROSS), wave, lane);
-        b.direct(lds + A::kBytes, ob, k_first, ends(left, B_ACROSS), wave, lane);
-        for (int t = 0; t < steps; ++t) {
-            __syncthreads();              // step t has come, and nobody reads the other half any more
-            left -= kStep;
-            direct_step<T, A, B, MF, NF>(lds + (t & 1) * kStage, lds + ((t + 1) & 1) * kStage, a, b, oa, ob, k_first + (uint32_t)(t + 1) * kStep,
-                                         ends(left, A_ACROSS), ends(left, B_ACROSS), t + 1 < steps, acc, wm, wn, wave, lane);
+        const int all = (int)(k_end - k_first);
+        const auto start = [&](int step) { return step < steps ? k_first + (uint32_t)step * kStep : k_first; };      // (past the end no address of it is used)
+        const auto left = [&](int step, bool across) { return all - step * kStep + (across ? 0 : extra); };
+        constexpr int kLoads = A::kPerThread + B::kPerThread;          // of a step, a wave
+        for (int t = 0; t < STAGES - 1; ++t) {
+            a.direct(lds + t * kStage, oa, start(t), left(t, A_ACROSS), wave, lane);
+            b.direct(lds + t * kStage + A::kBytes, ob, start(t), left(t, B_ACROSS), wave, lane);
         }
+        int cur = 0, next = STAGES - 1;
+        for (int t = 0; t < steps; ++t) {
+            wait_loads<(STAGES - 2) * kLoads>();
+            barrier_alone();              // step t has come for all waves, and nobody reads step t - 1 any more: step t + STAGES - 1 goes over it
+            // (steps past the end set out zeros, so that the count holds)
+            const int s = t + STAGES - 1;
+            direct_step<T, A, B, MF, NF, STAGES == 2 && BM == 128>(lds + cur * kStage, lds + next * kStage, a, b, oa, ob, start(s), left(s, A_ACROSS), left(s, B_ACROSS), acc, wm, wn, wave, lane);
+            cur = cur + 1 == STAGES ? 0 : cur + 1;
+            next = next + 1 == STAGES ? 0 : next + 1;
+        }
+        wait_loads<0>();
     } else {
         u32x4 ra[A::kPerThread], rb[B::kPerThread];
         a.load(ra, k_first, (int)(k_end - k_first), tid);
@@ -497,7 +519,7 @@ k_product(const ProductArgs p)
     }
 
     __syncthreads();
-    static_assert(BM / WM * (BN / WN) * 4 * NT / 64 / (BM / WM > 64 ? BM / WM / 64 : 1) <= 2 * kStage, "the sums fit");
+    static_assert(BM / WM * (BN / WN) * 4 * NT / 64 / (BM / WM > 64 ? BM / WM / 64 : 1) <= STAGES * kStage, "the sums fit");
     finish_wave<T, BM / WM, BN / WN, false>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
 }
 
@@ -508,10 +530,6 @@ k_product(const ProductArgs p)
 //   wait until step t + 1 has come and own reads of step t are done, barrier: nobody reads step t any more, all of step t + 1 is there;
 //   products (t, h1), meanwhile set out step t + 2 over step t and read (t + 1, h0).
 // So 64 KB are on their way at any time, for the length of a step.  Steps past the end set out zeros and are read but not multiplied.
-template <int COUNT> __device__ __forceinline__ void wait_loads()      // until at most COUNT vector memory accesses of the wave are on their way
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
-}
 __device__ __forceinline__ void meet()                                  // all waves' LDS reads and direct loads before here are done for all
 {
     __builtin_amdgcn_sched_barrier(0);

@@ -203,11 +203,11 @@ am_status launch_kernel(void (*kernel)(ProductArgs), ProductArgs &a, uint32_t ti
     return AM_OK;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool AA, bool BA, bool DIRECT>
+template <typename T, int BM, int BN, int WM, int WN, bool AA, bool BA, bool DIRECT, int STAGES>
 am_status launch_tiles(ProductArgs &a, hipStream_t stream)
 {
     static_assert(BM == BN, "square tiles");
-    return launch_kernel(am::k_product<T, BM, BN, WM, WN, AA, BA, DIRECT>, a, BM, 64 * WM * WN, 2u * (BM + BN) * 128u, stream);
+    return launch_kernel(am::k_product<T, BM, BN, WM, WN, AA, BA, DIRECT, STAGES>, a, BM, 64 * WM * WN, (uint32_t)STAGES * (BM + BN) * 128u, stream);
 }
 
 template <typename T, bool AA, bool BA, bool DIRECT>
@@ -216,11 +216,13 @@ am_status launch_shape(ProductArgs &a, const ProductPlan &p, hipStream_t stream)
     if constexpr (sizeof(T) == 2) {
         if (p.tile == 256) {
             if constexpr (DIRECT) return launch_kernel(am::k_product_large<AA, BA>, a, 256, 512, 131072, stream);
-            else return launch_tiles<T, 256, 256, 2, 4, AA, BA, DIRECT>(a, stream);
+            else return launch_tiles<T, 256, 256, 2, 4, AA, BA, DIRECT, 2>(a, stream);
         }
     }
-    if (p.tile == 64) return launch_tiles<T, 64, 64, 2, 2, AA, BA, DIRECT>(a, stream);
-    return launch_tiles<T, 128, 128, 2, 2, AA, BA, DIRECT>(a, stream);
+    if constexpr (DIRECT)
+        if (p.tile == 64 && p.stages == 4) return launch_tiles<T, 64, 64, 2, 2, AA, BA, DIRECT, 4>(a, stream);
+    if (p.tile == 64) return launch_tiles<T, 64, 64, 2, 2, AA, BA, DIRECT, 2>(a, stream);
+    return launch_tiles<T, 128, 128, 2, 2, AA, BA, DIRECT, 2>(a, stream);
 }
 
 template <typename T>

@@ -8,24 +8,25 @@ constexpr uint32_t kComputeUnits = 256;      // of an MI355X
 
 struct ProductPlan {
     uint32_t tile;         // 256, 128 or 64: both sides
+    uint32_t stages;       // steps of it that LDS holds: 2, or 4 of the smallest tile where few workgroups hide a load's way
     uint32_t splits;       // workgroups that share a tile's sum
     uint32_t split_k;      // of k for each, a multiple of a step
 };
 
 // The time of a product by what its workgroups take.  A workgroup's step (128 bytes of k of both operands) lasts `alone_us` by itself and
 // `share_us` for each workgroup of its compute unit where that is longer; `resident` of them run at a time; every workgroup costs `fixed_us` besides; a sum
-// that is split costs a launch and its parts' way through memory.  The constants fit 2200 timed products on an MI355X (16 to
+// that is split costs a launch, the host's 2 us for it and its parts' way through memory.  The constants fit 2900 timed products on an MI355X (16 to
 // 8192 rows, 128 to 8192 columns, one to eight replicas, 1 to 32 splits; bf16 and fp32, straight into LDS and through registers): what the rule
-// picks took 1.5 to 2.6 % more than the best of all on average, 20 % at worst (9 us against 7).
-struct TileCost { uint32_t tile, resident; double alone_us, share_us, fixed_us; };
-struct ProductCost { TileCost tiles[3]; uint32_t count; double join_us, join_tb_s; };
+// picks took 1.2 to 2.2 % more than the best of all on average, 29 % at worst (36 us against 28).
+struct TileCost { uint32_t tile, stages, resident; double alone_us, share_us, fixed_us; };
+struct ProductCost { TileCost tiles[4]; uint32_t count; double join_us, join_tb_s; };
 
 inline const ProductCost &product_cost(bool bf16, bool direct)
 {
-    static const ProductCost bf16_direct = {{{256, 1, 1.285, 1.285, 6.35}, {128, 2, 0.654, 0.472, 3.33}, {64, 4, 0.43, 0.195, 2.12}}, 3, 3.09, 4.1};
-    static const ProductCost bf16_staged = {{{256, 1, 2.355, 2.355, 5.09}, {128, 2, 0.895, 0.895, 3.85}, {64, 4, 0.568, 0.262, 1.89}}, 3, 3.9, 4.8};
-    static const ProductCost f32_direct = {{{128, 2, 2.04, 2.04, 4.44}, {64, 4, 0.681, 0.59, 2.73}}, 2, 3.86, 5.4};
-    static const ProductCost f32_staged = {{{128, 2, 2.36, 2.11, 4.33}, {64, 4, 0.752, 0.616, 2.57}}, 2, 3.9, 4.8};
+    static const ProductCost bf16_direct = {{{256, 2, 1, 1.26, 1.26, 6.45}, {128, 2, 2, 0.716, 0.497, 3.21}, {64, 2, 4, 0.371, 0.2, 2.2}, {64, 4, 2, 0.264, 0.188, 2.38}}, 4, 5.2, 4.3};
+    static const ProductCost bf16_staged = {{{256, 2, 1, 1.95, 1.95, 4.11}, {128, 2, 2, 0.882, 0.695, 3.1}, {64, 2, 4, 0.541, 0.253, 1.44}}, 3, 5.9, 3.5};
+    static const ProductCost f32_direct = {{{128, 2, 2, 2.23, 1.96, 3.45}, {64, 2, 4, 0.757, 0.573, 2.08}, {64, 4, 2, 0.625, 0.539, 2.37}}, 3, 5.9, 4.3};
+    static const ProductCost f32_staged = {{{128, 2, 2, 2.37, 2.13, 4.06}, {64, 2, 4, 0.738, 0.607, 2.5}}, 2, 5.7, 4.7};
     return bf16 ? (direct ? bf16_direct : bf16_staged) : (direct ? f32_direct : f32_staged);
 }
 
@@ -34,7 +35,7 @@ inline ProductPlan product_plan(bool bf16, bool direct, uint64_t replicas, uint6
 {
     const ProductCost &cost = product_cost(bf16, direct);
     const uint64_t step = bf16 ? 64 : 32, steps = (k + step - 1) / step;
-    ProductPlan best = {64, 1, (uint32_t)(steps * step)};
+    ProductPlan best = {64, 2, 1, (uint32_t)(steps * step)};
     double best_us = -1.;
     for (uint32_t i = 0; i < cost.count; ++i) {
         const TileCost &s = cost.tiles[i];
@@ -48,7 +49,7 @@ inline ProductPlan product_plan(bool bf16, bool direct, uint64_t replicas, uint6
             };
             double us = (double)rounds * round_us(s.resident) + (rest ? round_us(rest) : 0.);
             if (used > 1) us += cost.join_us + (double)(used + 1) * 4. * (double)(replicas * m) * (double)n / (cost.join_tb_s * 1e6);
-            if (best_us < 0. || us < best_us) { best_us = us; best = {s.tile, (uint32_t)used, (uint32_t)(each * step)}; }
+            if (best_us < 0. || us < best_us) { best_us = us; best = {s.tile, s.stages, (uint32_t)used, (uint32_t)(each * step)}; }
             if (tiles * splits > 4096) break;        // (more parts of a sum than workgroups can use)
         }
     }

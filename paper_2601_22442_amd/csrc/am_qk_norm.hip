@@ -143,7 +143,8 @@ am_status run(const am_qk_config &c, const am_qk_buffers &b, hipStream_t stream)
         a.parts[w] = s.parts[w];
         if (a.want_gain[w]) a.partial[w] = partials(c, b, s, w);
     }
-    if (s.v == 8) launch<T, 8, 1, BACKWARD ? 2 : 4, BACKWARD>(a, c, s, stream);            // 32 lanes at most: 256 pairs
+    if (s.v == 8 && s.block == 1) launch<T, 8, 1, 1, BACKWARD>(a, c, s, stream);          // few heads: the shorter code
+    else if (s.v == 8) launch<T, 8, 1, BACKWARD ? 2 : 4, BACKWARD>(a, c, s, stream);       // 32 lanes at most: 256 pairs
     else if (s.times == 1) launch<T, 1, 1, 4, BACKWARD>(a, c, s, stream);
     else launch<T, 1, 4, 2, BACKWARD>(a, c, s, stream);                                   // 64 lanes, up to four pairs each
     AM_HIP(hipGetLastError());
