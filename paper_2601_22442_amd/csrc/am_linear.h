@@ -16,7 +16,7 @@
 
 namespace am {
 
-constexpr uint32_t kLinearMaxReplicas = 32;
+constexpr uint32_t kLinearMaxReplicas = 32;      // (two products' arguments stay below 4 KB)
 constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4;
 
 // ---------------------------------------------------------------------------------------------
@@ -88,6 +88,7 @@ struct ProductArgs {
     float *partial;                            // [split][replica][m][n] when splits > 1
     ProductArrays of[kLinearMaxReplicas];
 };
+static_assert(2 * sizeof(ProductArgs) + 8 < 4096, "kernel arguments");
 
 template <int ACT, int N> __device__ __forceinline__ void act_all(F8 (&x)[N])
 {
@@ -443,18 +444,15 @@ __device__ __forceinline__ void barrier_alone()
 // BM x BN tile, WM x WN waves, each BM / WM by BN / WN.  LDS holds STAGES steps of both operands, one read while the others are on their
 // way; one barrier a step.  DIRECT: straight from memory, else through registers (two stages).
 template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int STAGES>
-__global__ void __launch_bounds__(64 * WM * WN, 2)
-k_product(const ProductArgs p)
+__device__ __forceinline__ void product_tile(const ProductArgs &p, uint32_t block, uint32_t blocks, char *lds)
 {
     constexpr int NT = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
     using A = Operand<T, BM, NT, A_ACROSS, 8>;
     using B = Operand<T, BN, NT, B_ACROSS, 8>;
     constexpr int kStep = A::kStep;
     constexpr int kStage = A::kBytes + B::kBytes;
-    extern __shared__ __align__(16) char lds[];
-
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Where w = where(p, blockIdx.x, gridDim.x);
+    const Where w = where(p, block, blocks);
     const uint32_t m0 = w.tile_m * BM, n0 = w.tile_n * BN;
     const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     const uint32_t k_first = w.split * p.split_k;
@@ -521,6 +519,27 @@ k_product(const ProductArgs p)
     __syncthreads();
     static_assert(BM / WM * (BN / WN) * 4 * NT / 64 / (BM / WM > 64 ? BM / WM / 64 : 1) <= STAGES * kStage, "the sums fit");
     finish_wave<T, BM / WM, BN / WN, false>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
+}
+
+template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int STAGES>
+__global__ void __launch_bounds__(64 * WM * WN, 2)
+k_product(const ProductArgs p)
+{
+    extern __shared__ __align__(16) char lds[];
+    product_tile<T, BM, BN, WM, WN, A_ACROSS, B_ACROSS, DIRECT, STAGES>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// The two products of a backward call, which need nothing of each other, in one launch: together they leave fewer compute units
+// without work in the last round, and one launch less.  Workgroups below `first` take dz w (dw_first: dz^T x), the others the other.
+template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int STAGES>
+__global__ void __launch_bounds__(64 * WM * WN, 2)
+k_product_pair(const ProductArgs dx, const ProductArgs dw, uint32_t first, uint32_t dw_first)
+{
+    extern __shared__ __align__(16) char lds[];
+    const bool low = blockIdx.x < first;
+    const uint32_t block = low ? blockIdx.x : blockIdx.x - first, blocks = low ? first : gridDim.x - first;
+    if (low != (dw_first != 0u)) product_tile<T, BM, BN, WM, WN, false, true, DIRECT, STAGES>(dx, block, blocks, lds);
+    else product_tile<T, BM, BN, WM, WN, true, true, DIRECT, STAGES>(dw, block, blocks, lds);
 }
 
 // The 256 x 256 tile of bf16: eight waves of 128 x 64, two to a SIMD.  Steps of 128 bytes of k (whole

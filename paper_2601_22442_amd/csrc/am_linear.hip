@@ -119,6 +119,7 @@ Source packed(const am_linear_config &c, const Source &s, char *to)
 }
 
 struct Planned {
+    double us;                   // by the measured times
     ProductPlan cut;
     bool direct, pack_a, pack_b;
     uint64_t pack_a_bytes, pack_b_bytes, partial_bytes, total;
@@ -141,8 +142,10 @@ Planned plan_product(const am_linear_config &c, uint64_t m, uint64_t n, uint64_t
         if (!p.direct || staged_us <= direct_us) {
             p.direct = p.pack_a = p.pack_b = false;
             p.cut = staged;
+            direct_us = staged_us;
         }
     }
+    p.us = direct_us;
     if (p.pack_a) p.pack_a_bytes = c.replicas * packed_bytes(c, a);
     if (p.pack_b) p.pack_b_bytes = c.replicas * packed_bytes(c, b);
     if (p.cut.splits > 1) p.partial_bytes = up256(4u * p.cut.splits * c.replicas * m * n);
@@ -162,6 +165,7 @@ struct PlannedBackward {
     uint64_t dz_bytes, sums_bytes, total;
     uint32_t rows_per_part, parts;
     Planned dx, dw;
+    bool pair;                   // both products in one launch
 };
 PlannedBackward plan_backward(const am_linear_config &c, const am_linear_buffers &b, char *workspace)
 {
@@ -177,6 +181,31 @@ PlannedBackward plan_backward(const am_linear_config &c, const am_linear_buffers
     if (b.dx) s.dx = plan_product(c, c.rows, c.in, c.out, s.dz, source(c, b.w, c.out, c.in, 0));
     if (b.dw) s.dw = plan_product(c, c.out, c.in, c.rows, s.dz, source(c, b.x, c.rows, c.in, c.x_stride));
     s.total = s.dz_bytes + s.sums_bytes + (s.dx.total > s.dw.total ? s.dx.total : s.dw.total);
+    if (!b.dx || !b.dw) return s;
+    // one launch for both where that is faster than one after the other (3 us: a launch between)
+    const am_host::Extent ex = {c.rows, c.in, c.out}, ew = {c.out, c.in, c.rows};
+    const Source w = source(c, b.w, c.out, c.in, 0), x = source(c, b.x, c.rows, c.in, c.x_stride);
+    double apart_us = s.dx.us + s.dw.us + 3.;
+    for (int direct = 1; direct >= 0; --direct) {
+        ProductPlan px, pw;
+        double us;
+        const bool pack_w = direct && !w.in_chunks, pack_x = direct && !x.in_chunks;
+        if (direct && (!s.dz.in_chunks || c.in >= (1ull << 22) - 8u)) continue;
+        if (!am_host::pair_plan(c.dtype == AM_BF16, direct != 0, c.replicas, ex, ew, &px, &pw, &us)) continue;
+        if (pack_w) us += am_host::pack_us(c.replicas * packed_bytes(c, w));
+        if (pack_x) us += am_host::pack_us(c.replicas * packed_bytes(c, x));
+        if (us >= apart_us) continue;
+        apart_us = us;
+        s.pair = true;
+        s.dx = Planned{}; s.dw = Planned{};
+        s.dx.cut = px; s.dw.cut = pw;
+        s.dx.direct = s.dw.direct = direct != 0;
+        s.dx.pack_b = pack_w; s.dw.pack_b = pack_x;
+        if (pack_w) s.dx.pack_b_bytes = c.replicas * packed_bytes(c, w);
+        if (pack_x) s.dw.pack_b_bytes = c.replicas * packed_bytes(c, x);
+        s.dx.total = s.dx.pack_b_bytes; s.dw.total = s.dw.pack_b_bytes;
+        s.total = s.dz_bytes + s.sums_bytes + s.dx.total + s.dw.total;
+    }
     return s;
 }
 
@@ -238,9 +267,10 @@ am_status pack(const am_linear_config &c, const Source &from, const Source &to, 
     return AM_OK;
 }
 
-// The product a plan describes: args holds C, its epilogue and m, n, k.  ACROSS: k runs across the operand's rows.
+// The operands of the product a plan describes, moved to aligned rows in `space` where it says so; args holds C, its epilogue and m, n, k.
+// AA, BA: k runs across the operand's rows.
 template <typename T, bool AA, bool BA>
-am_status launch_product(const am_linear_config &c, ProductArgs &args, const Planned &p, Source a, Source b, char *space, hipStream_t stream)
+am_status set_operands(const am_linear_config &c, ProductArgs &args, const Planned &p, Source a, Source b, char *space, hipStream_t stream)
 {
     if (p.pack_a) {
         const Source t = packed(c, a, space);
@@ -265,12 +295,48 @@ am_status launch_product(const am_linear_config &c, ProductArgs &args, const Pla
     if (!AA) whole = a.zeros_to;
     if (!BA && b.zeros_to < whole) whole = b.zeros_to;
     args.k_whole = p.direct && whole != UINT64_MAX ? (uint32_t)whole : args.k;
-    const am_status s = p.direct ? launch_shape<T, AA, BA, true>(args, p.cut, stream) : launch_shape<T, AA, BA, false>(args, p.cut, stream);
+    return AM_OK;
+}
+
+template <typename T, bool AA, bool BA>
+am_status launch_product(const am_linear_config &c, ProductArgs &args, const Planned &p, const Source &a, const Source &b, char *space, hipStream_t stream)
+{
+    am_status s = set_operands<T, AA, BA>(c, args, p, a, b, space, stream);
+    if (s != AM_OK) return s;
+    s = p.direct ? launch_shape<T, AA, BA, true>(args, p.cut, stream) : launch_shape<T, AA, BA, false>(args, p.cut, stream);
     if (s != AM_OK || p.cut.splits <= 1) return s;
     const uint64_t blocks = ((uint64_t)((args.n + 7u) / 8u) * args.m + 255u) / 256u;
     am::k_product_join<T><<<dim3((uint32_t)(blocks < 4096u ? blocks : 4096u), 1, args.replicas), 256, 0, stream>>>(args);
     AM_HIP(hipGetLastError());
     return AM_OK;
+}
+
+// dx and dw in one launch, the one with the longer sums first
+template <typename T, int TILE, bool DIRECT, int STAGES>
+am_status launch_pair(ProductArgs &dx, ProductArgs &dw, hipStream_t stream)
+{
+    uint64_t blocks[2];
+    ProductArgs *const args[2] = {&dx, &dw};
+    for (int i = 0; i < 2; ++i) {
+        args[i]->tiles_m = (args[i]->m + TILE - 1) / TILE;
+        args[i]->tiles_n = (args[i]->n + TILE - 1) / TILE;
+        blocks[i] = (uint64_t)args[i]->tiles_m * args[i]->tiles_n * args[i]->replicas;
+    }
+    if (blocks[0] + blocks[1] >= kMaxExtent) return fail(AM_EINVAL, "products of %llu tiles are too large for one launch", (unsigned long long)(blocks[0] + blocks[1]));
+    const uint32_t dw_first = dw.k > dx.k, first = (uint32_t)blocks[dw_first];
+    am::k_product_pair<T, TILE, TILE, 2, 2, DIRECT, STAGES><<<(uint32_t)(blocks[0] + blocks[1]), 256, STAGES * 2u * TILE * 128u, stream>>>(dx, dw, first, dw_first);
+    AM_HIP(hipGetLastError());
+    return AM_OK;
+}
+
+template <typename T>
+am_status launch_pair_shape(ProductArgs &dx, ProductArgs &dw, const Planned &p, hipStream_t stream)
+{
+    if (p.direct) {
+        if (p.cut.tile == 64) return p.cut.stages == 4 ? launch_pair<T, 64, true, 4>(dx, dw, stream) : launch_pair<T, 64, true, 2>(dx, dw, stream);
+        return launch_pair<T, 128, true, 2>(dx, dw, stream);
+    }
+    return p.cut.tile == 64 ? launch_pair<T, 64, false, 2>(dx, dw, stream) : launch_pair<T, 128, false, 2>(dx, dw, stream);
 }
 
 template <typename T>
@@ -352,25 +418,30 @@ am_status backward(const am_linear_config &c, const am_linear_buffers &b, const 
             AM_HIP(hipGetLastError());
         }
     }
-    ProductArgs a;
+    ProductArgs dx, dw;
+    const Source w = b.dx ? source(c, b.w, c.out, c.in, 0) : Source{}, x = b.dw ? source(c, b.x, c.rows, c.in, c.x_stride) : Source{};
     if (b.dx) {
-        std::memset(&a, 0, sizeof a);
-        for (uint32_t i = 0; i < c.replicas; ++i) a.of[i].c = b.dx[i];
-        a.m = (uint32_t)c.rows; a.n = (uint32_t)c.in; a.k = (uint32_t)c.out;
-        a.ldc = (uint32_t)or_dense(c.dx_stride, c.in);
-        const am_status s = launch_product<T, false, true>(c, a, sp.dx, sp.dz, source(c, b.w, c.out, c.in, 0), space, stream);
-        if (s != AM_OK) return s;
+        std::memset(&dx, 0, sizeof dx);
+        for (uint32_t i = 0; i < c.replicas; ++i) dx.of[i].c = b.dx[i];
+        dx.m = (uint32_t)c.rows; dx.n = (uint32_t)c.in; dx.k = (uint32_t)c.out;
+        dx.ldc = (uint32_t)or_dense(c.dx_stride, c.in);
     }
     if (b.dw) {
-        std::memset(&a, 0, sizeof a);
-        for (uint32_t i = 0; i < c.replicas; ++i) { a.of[i].c = b.dw[i]; if (accumulate) a.of[i].add = b.dw[i]; }
-        a.m = (uint32_t)c.out; a.n = (uint32_t)c.in; a.k = (uint32_t)c.rows;
-        a.ldc = a.ldadd = (uint32_t)c.in;
-        a.out_f32 = sizeof(O) == 4;
-        const am_status s = launch_product<T, true, true>(c, a, sp.dw, sp.dz, source(c, b.x, c.rows, c.in, c.x_stride), space, stream);
-        if (s != AM_OK) return s;
+        std::memset(&dw, 0, sizeof dw);
+        for (uint32_t i = 0; i < c.replicas; ++i) { dw.of[i].c = b.dw[i]; if (accumulate) dw.of[i].add = b.dw[i]; }
+        dw.m = (uint32_t)c.out; dw.n = (uint32_t)c.in; dw.k = (uint32_t)c.rows;
+        dw.ldc = dw.ldadd = (uint32_t)c.in;
+        dw.out_f32 = sizeof(O) == 4;
     }
-    return AM_OK;
+    am_status s = AM_OK;
+    if (sp.pair) {
+        s = set_operands<T, false, true>(c, dx, sp.dx, sp.dz, w, space, stream);
+        if (s == AM_OK) s = set_operands<T, true, true>(c, dw, sp.dw, sp.dz, x, space + sp.dx.total, stream);
+        return s == AM_OK ? launch_pair_shape<T>(dx, dw, sp.dx, stream) : s;
+    }
+    if (b.dx) s = launch_product<T, false, true>(c, dx, sp.dx, sp.dz, w, space, stream);
+    if (b.dw && s == AM_OK) s = launch_product<T, true, true>(c, dw, sp.dw, sp.dz, x, space, stream);
+    return s;
 }
 
 }  // namespace

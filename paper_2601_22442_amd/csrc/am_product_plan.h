@@ -57,6 +57,33 @@ inline ProductPlan product_plan(bool bf16, bool direct, uint64_t replicas, uint6
     return best;
 }
 
+// Two products in one launch, unsplit, with one tile: the time of their steps over all compute units, and half the longer workgroup's for the
+// end.  Returns false where a tile that both can take does not exist (the 256 tile has no such kernel).
+struct Extent { uint64_t m, n, k; };
+inline bool pair_plan(bool bf16, bool direct, uint64_t replicas, const Extent &a, const Extent &b, ProductPlan *out_a, ProductPlan *out_b, double *out_us)
+{
+    const ProductCost &cost = product_cost(bf16, direct);
+    const uint64_t step = bf16 ? 64 : 32, steps_a = (a.k + step - 1) / step, steps_b = (b.k + step - 1) / step;
+    bool found = false;
+    for (uint32_t i = 0; i < cost.count; ++i) {
+        const TileCost &s = cost.tiles[i];
+        if (s.tile == 256) continue;
+        const double tiles_a = (double)(((a.m + s.tile - 1) / s.tile) * ((a.n + s.tile - 1) / s.tile) * replicas);
+        const double tiles_b = (double)(((b.m + s.tile - 1) / s.tile) * ((b.n + s.tile - 1) / s.tile) * replicas);
+        const double own_a = (double)steps_a * s.alone_us + s.fixed_us, own_b = (double)steps_b * s.alone_us + s.fixed_us, longest = own_a > own_b ? own_a : own_b;
+        const double fixed = s.fixed_us / s.resident;
+        const double all = (tiles_a * ((double)steps_a * s.share_us + fixed) + tiles_b * ((double)steps_b * s.share_us + fixed)) / kComputeUnits + 0.5 * longest;
+        const double us = all > longest ? all : longest;
+        if (!found || us < *out_us) {
+            found = true;
+            *out_us = us;
+            *out_a = {s.tile, s.stages, 1, (uint32_t)(steps_a * step)};
+            *out_b = {s.tile, s.stages, 1, (uint32_t)(steps_b * step)};
+        }
+    }
+    return found;
+}
+
 // Time of copying an operand to aligned rows first: a launch, and both ways at what a copy of strided rows reaches.
 inline double pack_us(uint64_t bytes) { return 3.5 + 2. * (double)bytes / 4e6; }
 
