@@ -12,6 +12,8 @@
 // The matrix instruction takes B as its first operand, so that a lane ends with four neighbouring n of one m.  The epilogue passes
 // them through LDS, wave by wave, so that eight lanes read and write 128 bytes side by side.
 #pragma once
+#include <type_traits>
+
 #include "am_elem.h"
 
 namespace am {
@@ -259,6 +261,8 @@ struct Operand {
             }
         }
     }
+    // FULL: the step lies within k
+    template <bool FULL = false>
     __device__ __forceinline__ void direct(char *lds, const uint32_t (&offset)[kPerThread], uint32_t k0, int k_left, int wave, int lane) const
     {
         const char *from = reinterpret_cast<const char *>(base + (ACROSS ? (uint64_t)k0 * ld : (uint64_t)k0));
@@ -266,7 +270,7 @@ struct Operand {
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
             const char *at = from + offset[i];
-            if (k_left < kStep) {                 // (the last step alone)
+            if (!FULL && k_left < kStep) {
                 const uint32_t q = (uint32_t)((wave * kPerThread + i) * 64 + lane);
                 const int k = ACROSS ? (int)(q / kRowChunks) : turned((int)(q / S), (int)(q % S)) * kChunk<T>;
                 at = k < k_left ? at : reinterpret_cast<const char *>(&zero_chunk);
@@ -416,13 +420,13 @@ __device__ __forceinline__ void products(const char *__restrict__ cur, f32x4 (&a
 }
 
 // The next step's chunks set out for `next`, then the products of the step in `cur`.
-template <typename T, typename A, typename B, int MF, int NF, bool EARLY>
+template <typename T, typename A, typename B, int MF, int NF, bool EARLY, bool FULL>
 __device__ __forceinline__ void direct_step(const char *__restrict__ cur, char *__restrict__ next, const A &a, const B &b,
                                             const uint32_t (&oa)[A::kPerThread], const uint32_t (&ob)[B::kPerThread], uint32_t k0, int ka, int kb,
                                             f32x4 (&acc)[MF][NF], int wm, int wn, int wave, int lane)
 {
-    a.direct(next, oa, k0, ka, wave, lane);
-    b.direct(next + A::kBytes, ob, k0, kb, wave, lane);
+    a.template direct<FULL>(next, oa, k0, ka, wave, lane);
+    b.template direct<FULL>(next + A::kBytes, ob, k0, kb, wave, lane);
     // With two stages of the 128 tile the loads go first: left to the compiler they went behind the products where B lies across
     // (38 us for 32 us of 3 x 1112 x 2304 -> 1152).  Deeper stages of the small tile have time, and lose up to 10 % by it.
     if constexpr (EARLY) __builtin_amdgcn_sched_barrier(0);
@@ -483,16 +487,19 @@ __device__ __forceinline__ void product_tile(const ProductArgs &p, uint32_t bloc
             a.direct(lds + t * kStage, oa, start(t), left(t, A_ACROSS), wave, lane);
             b.direct(lds + t * kStage + A::kBytes, ob, start(t), left(t, B_ACROSS), wave, lane);
         }
-        int cur = 0, next = STAGES - 1;
-        for (int t = 0; t < steps; ++t) {
+        int cur = 0, next = STAGES - 1, t = 0;
+        const auto step = [&](auto full) {
             wait_loads<(STAGES - 2) * kLoads>();
             barrier_alone();              // step t has come for all waves, and nobody reads step t - 1 any more: step t + STAGES - 1 goes over it
-            // (steps past the end set out zeros, so that the count holds)
             const int s = t + STAGES - 1;
-            direct_step<T, A, B, MF, NF, STAGES == 2 && BM == 128>(lds + cur * kStage, lds + next * kStage, a, b, oa, ob, start(s), left(s, A_ACROSS), left(s, B_ACROSS), acc, wm, wn, wave, lane);
+            direct_step<T, A, B, MF, NF, STAGES == 2 && BM == 128, decltype(full)::value>(lds + cur * kStage, lds + next * kStage, a, b, oa, ob, start(s), left(s, A_ACROSS),
+                                                                                        left(s, B_ACROSS), acc, wm, wn, wave, lane);
             cur = cur + 1 == STAGES ? 0 : cur + 1;
             next = next + 1 == STAGES ? 0 : next + 1;
-        }
+        };
+        // (the steps that set out a whole step, without a question for each chunk, then the last ones, which set out zeros past the end, so that the count holds)
+        for (; t + STAGES < steps; ++t) step(std::true_type{});
+        for (; t < steps; ++t) step(std::false_type{});
         wait_loads<0>();
     } else {
         u32x4 ra[A::kPerThread], rb[B::kPerThread];
@@ -578,13 +585,13 @@ __device__ __forceinline__ void interleave()
 }
 
 // `over` is written by direct loads while `from` is read
-template <typename T, typename A, typename B, int MF, int NF>
+template <typename T, typename A, typename B, int MF, int NF, bool FULL>
 __device__ __forceinline__ void second_half(const char *__restrict__ from, char *__restrict__ over, const A &a, const B &b, const uint32_t (&oa)[A::kPerThread],
                                             const uint32_t (&ob)[B::kPerThread], uint32_t k0, int ka, int kb, const u32x4 (&fa)[MF], const u32x4 (&fb)[NF],
                                             u32x4 (&na)[MF], u32x4 (&nb)[NF], f32x4 (&acc)[MF][NF], int wm, int wn, int wave, int lane)
 {
-    a.direct(over, oa, k0, ka, wave, lane);
-    b.direct(over + A::kBytes, ob, k0, kb, wave, lane);
+    a.template direct<FULL>(over, oa, k0, ka, wave, lane);
+    b.template direct<FULL>(over + A::kBytes, ob, k0, kb, wave, lane);
     fetch_half<T, A, B, MF, NF>(from, 0, na, nb, wm, wn, lane);
     multiply_half<T, MF, NF>(fa, fb, acc);
     interleave<MF * (A::kAcross ? 2 : 1) + NF * (B::kAcross ? 2 : 1), true>();
@@ -635,15 +642,19 @@ k_product_large(const ProductArgs p)
     __builtin_amdgcn_sched_barrier(0);
     u32x4 fa0[MF], fb0[NF], fa1[MF], fb1[NF];
     fetch_half<T, A, B, MF, NF>(lds, 0, fa0, fb0, wm, wn, lane);
-    for (int t = 0; t < steps; ++t) {
+    // (the steps that set out a whole step, without a question for each chunk, then the last ones)
+    int t = 0;
+    const auto step = [&](auto full) {
         char *cur = lds + (t & 1) * kStage, *next = lds + ((t + 1) & 1) * kStage;
         fetch_half<T, A, B, MF, NF>(cur, 1, fa1, fb1, wm, wn, lane);
         multiply_half<T, MF, NF>(fa0, fb0, acc);
         interleave<MF * (A_ACROSS ? 2 : 1) + NF * (B_ACROSS ? 2 : 1), false>();
         meet();
-        second_half<T, A, B, MF, NF>(next, cur, a, b, oa, ob, start(t + 2), left(t + 2, A_ACROSS), left(t + 2, B_ACROSS), fa1, fb1, fa0, fb0, acc, wm, wn, wave, lane);
+        second_half<T, A, B, MF, NF, decltype(full)::value>(next, cur, a, b, oa, ob, start(t + 2), left(t + 2, A_ACROSS), left(t + 2, B_ACROSS), fa1, fb1, fa0, fb0, acc, wm, wn, wave, lane);
         __builtin_amdgcn_sched_barrier(0);
-    }
+    };
+    for (; t + 3 < steps; ++t) step(std::true_type{});
+    for (; t < steps; ++t) step(std::false_type{});
     wait_loads<0>();
     __syncthreads();
     finish_wave<T, 128, 64, true>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);

@@ -137,18 +137,23 @@ k_norm_parts(const NormTable a, double *__restrict__ partial)
     if (threadIdx.x == 0) partial[(uint64_t)rep * a.parts_all + a.parts_before + part] = sum;
 }
 
-// one workgroup a replica: its parts in a fixed order, the norm and the factor
-__global__ void __launch_bounds__(kNormThreads)
-k_norm_finish(const double *__restrict__ partial, uint32_t parts, double max_norm, float *__restrict__ norm, float *__restrict__ factor)
+// What follows from a replica's parts: the same sum, in the same order, wherever it is formed.  By a whole workgroup.
+struct NormAndFactor { float norm, factor; };
+__device__ __forceinline__ NormAndFactor norm_of_parts(const double *__restrict__ partial, uint32_t parts, double max_norm)
 {
     double acc = 0.;
 #pragma unroll 8
-    for (uint32_t i = threadIdx.x; i < parts; i += kNormThreads) acc += partial[(uint64_t)blockIdx.x * parts + i];
+    for (uint32_t i = threadIdx.x; i < parts; i += kNormThreads) acc += partial[i];
     const double n = sqrt(sum_of_workgroup(acc));
-    if (threadIdx.x == 0) {
-        norm[blockIdx.x] = (float)n;
-        factor[blockIdx.x] = n <= max_norm ? 1.f : (float)(max_norm / n);
-    }
+    return {(float)n, n <= max_norm ? 1.f : (float)(max_norm / n)};
+}
+
+// one workgroup a replica
+__global__ void __launch_bounds__(kNormThreads)
+k_norm_finish(const double *__restrict__ partial, uint32_t parts, double max_norm, float *__restrict__ norm, float *__restrict__ factor)
+{
+    const NormAndFactor r = norm_of_parts(partial + (uint64_t)blockIdx.x * parts, parts, max_norm);
+    if (threadIdx.x == 0) { norm[blockIdx.x] = r.norm; factor[blockIdx.x] = r.factor; }
 }
 
 template <typename T, typename O>
@@ -163,14 +168,23 @@ __device__ __forceinline__ void scale_part(const T *g, O *out, uint64_t first, u
     });
 }
 
-// grid = (parts, replicas); without flat arrays in place, where a factor of one leaves nothing to do
+// grid = (parts, replicas); without flat arrays in place, where a factor of one leaves nothing to do.  FINISH: every workgroup forms its
+// replica's factor itself, and the first ones of the call's first launch write it down.
+template <bool FINISH>
 __global__ void __launch_bounds__(kNormThreads)
-k_norm_scale(const NormTable a, const float *__restrict__ factors)
+k_norm_scale(const NormTable a, const double *__restrict__ partial, double max_norm, float *__restrict__ norm, float *__restrict__ factors)
 {
     const uint32_t part = blockIdx.x, rep = blockIdx.y, t = tensor_of(a, part);
+    float factor;
+    if constexpr (FINISH) {
+        const NormAndFactor r = norm_of_parts(partial + (uint64_t)rep * a.parts_all, a.parts_all, max_norm);
+        factor = r.factor;
+        if (part == 0u && a.parts_before == 0u && threadIdx.x == 0) { norm[rep] = r.norm; factors[rep] = r.factor; }
+    } else {
+        factor = factors[rep];
+    }
     const uint64_t first = (uint64_t)(part - a.first_part[t]) * a.part_elements;
     const uint64_t last = a.numel[t] - first < a.part_elements ? a.numel[t] : first + a.part_elements;
-    const float factor = factors[rep];
     void *g = a.g[rep * a.tensors + t];
     const bool bf16 = (a.bf16 >> t) & 1u;
     if (!a.out[rep]) {

@@ -12,6 +12,8 @@ using am_host::fail;
 
 constexpr uint64_t kMaxElements = 1ull << 40;
 constexpr uint32_t kMaxTensors = 1u << 20;
+// Up to here every workgroup of the scaling pass adds up its replica's parts itself, which saves a launch.
+constexpr uint64_t kPartsToJoinThere = 1024;
 
 struct Cut {
     uint32_t part_elements;
@@ -102,7 +104,7 @@ am_status each_table(const am_norm_config &c, const Cut &cut, const void *const 
     return AM_OK;
 }
 
-am_status norms(const am_norm_config &c, const Cut &cut, const void *const *grads, void *const *out, float *norm, float *factor, double *partial, hipStream_t stream)
+am_status norms(const am_norm_config &c, const Cut &cut, const void *const *grads, void *const *out, float *norm, float *factor, double *partial, bool finish, hipStream_t stream)
 {
     const am_status s = each_table(c, cut, grads, out, [&](const am::NormTable &a, uint32_t parts) {
         const dim3 grid(parts, c.replicas);
@@ -110,7 +112,7 @@ am_status norms(const am_norm_config &c, const Cut &cut, const void *const *grad
         else if (c.out_dtype == AM_F32) am::k_norm_parts<1><<<grid, am::kNormThreads, 0, stream>>>(a, partial);
         else am::k_norm_parts<2><<<grid, am::kNormThreads, 0, stream>>>(a, partial);
     });
-    if (s != AM_OK) return s;
+    if (s != AM_OK || !finish) return s;
     am::k_norm_finish<<<c.replicas, am::kNormThreads, 0, stream>>>(partial, (uint32_t)cut.parts, c.max_norm, norm, factor);
     AM_HIP(hipGetLastError());
     return AM_OK;
@@ -154,7 +156,7 @@ am_status am_grad_norm(const am_norm_config *cfg, const void *const *grads, void
     Cut cut;
     const am_status s = prepare(cfg, grads, out, dev_norm, dev_factor, workspace, workspace_bytes, &cut);
     if (s != AM_OK) return s;
-    return norms(*cfg, cut, grads, out, dev_norm, dev_factor, static_cast<double *>(workspace), static_cast<hipStream_t>(hip_stream));
+    return norms(*cfg, cut, grads, out, dev_norm, dev_factor, static_cast<double *>(workspace), true, static_cast<hipStream_t>(hip_stream));
 }
 
 am_status am_clip_grads(const am_norm_config *cfg, void *const *grads, void *const *out, float *dev_norm, float *dev_factor,
@@ -165,10 +167,14 @@ am_status am_clip_grads(const am_norm_config *cfg, void *const *grads, void *con
     am_status s = prepare(cfg, in, out, dev_norm, dev_factor, workspace, workspace_bytes, &cut);
     if (s != AM_OK) return s;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    s = norms(*cfg, cut, in, nullptr, dev_norm, dev_factor, static_cast<double *>(workspace), stream);
+    double *partial = static_cast<double *>(workspace);
+    const bool finish_there = cut.parts != 0 && cut.parts <= kPartsToJoinThere;
+    s = norms(*cfg, cut, in, nullptr, dev_norm, dev_factor, partial, !finish_there, stream);
     if (s != AM_OK) return s;
     return each_table(*cfg, cut, in, out, [&](const am::NormTable &a, uint32_t parts) {
-        am::k_norm_scale<<<dim3(parts, cfg->replicas), am::kNormThreads, 0, stream>>>(a, dev_factor);
+        const dim3 grid(parts, cfg->replicas);
+        if (finish_there) am::k_norm_scale<true><<<grid, am::kNormThreads, 0, stream>>>(a, partial, cfg->max_norm, dev_norm, dev_factor);
+        else am::k_norm_scale<false><<<grid, am::kNormThreads, 0, stream>>>(a, partial, cfg->max_norm, dev_norm, dev_factor);
     });
 }
 

@@ -87,13 +87,12 @@ inline bool pair_plan(bool bf16, bool direct, uint64_t replicas, const Extent &a
 // Time of copying an operand to aligned rows first: a launch, and both ways at what a copy of strided rows reaches.
 inline double pack_us(uint64_t bytes) { return 3.5 + 2. * (double)bytes / 4e6; }
 
-// Rows for each workgroup of the column sums: some 2048 workgroups, 64 rows at least.
+// Rows for each workgroup of the column sums: some 4096 workgroups, 32 rows (one turn) at least.
 inline void column_parts(uint64_t replicas, uint64_t m, uint64_t n, uint32_t *rows_per_part, uint32_t *parts)
 {
     const uint64_t across = ((n + 255) / 256) * replicas;
-    uint64_t want = across >= 2048 ? 1 : 2048 / across;
-    uint64_t rows = (m + want - 1) / want;
-    rows = rows < 64 ? 64 : rows;
+    const uint64_t want = across >= 4096 ? 1 : 4096 / across;
+    uint64_t rows = ((m + want - 1) / want + 31) / 32 * 32;
     if ((m + rows - 1) / rows > 65535) rows = (m + 65534) / 65535;
     *rows_per_part = (uint32_t)rows;
     *parts = (uint32_t)((m + rows - 1) / rows);
