@@ -679,6 +679,68 @@ k_product_join(const ProductArgs p)
 }
 
 // ---------------------------------------------------------------------------------------------
+// x w^T of a few rows: a weight is used so few times that reading it is all that counts
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ float sum_of_wave(float x)
+{
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xB1, 0xF, 0xF, true));         // quad_perm [1, 0, 3, 2]
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4E, 0xF, 0xF, true));         // quad_perm [2, 3, 0, 1]
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xF, 0xF, true));        // row_half_mirror
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, 0xF, 0xF, true));        // row_mirror
+    x += __shfl_xor(x, 16, 64);
+    return x + __shfl_xor(x, 32, 64);
+}
+
+// A workgroup takes NR rows of w and all MR rows of x (rows past the end repeat the last ones and are left out at the end); its threads go
+// through k side by side, eight elements each, the loads of a turn on their way together.  grid = (rows of w / NR, replicas)
+template <typename T, int MR, int NR>
+__global__ void __launch_bounds__(256)
+k_few_rows(const ProductArgs p)
+{
+    __shared__ float part[4][MR * NR];
+    const ProductArrays of = p.of[blockIdx.y];
+    const uint32_t n0 = blockIdx.x * NR, tid = threadIdx.x;
+    const T *w[NR], *x[MR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) w[r] = static_cast<const T *>(of.b) + (uint64_t)(n0 + r < p.n ? n0 + r : p.n - 1u) * p.ldb;
+#pragma unroll
+    for (int m = 0; m < MR; ++m) x[m] = static_cast<const T *>(of.a) + (uint64_t)((uint32_t)m < p.m ? m : p.m - 1u) * p.lda;
+    float acc[MR][NR];
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) acc[m][r] = 0.f;
+    for (uint32_t k = tid * 8u; k < p.k; k += 2048u) {
+        const int valid = p.k - k < 8u ? (int)(p.k - k) : 8;
+        F8 fw[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) fw[r] = load8(w[r] + k, valid);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+            const F8 fx = load8(x[m] + k, valid);
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[m][r] = __builtin_fmaf(fx.v[j], fw[r].v[j], acc[m][r]);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const float s = sum_of_wave(acc[m][r]);
+            if ((tid & 63u) == 0u) part[tid >> 6][m * NR + r] = s;
+        }
+    __syncthreads();
+    const uint32_t m = tid / NR, n = n0 + tid % NR;
+    if (tid >= MR * NR || m >= p.m || n >= p.n) return;
+    F8 y[1] = {};
+    y[0].v[0] = part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid];
+    const uint32_t rows[1] = {m};
+    finish8<T, 1, false, false>(Finish(p, blockIdx.y), rows, p.m, n, 1, bias8<T>(p, blockIdx.y, n, 1), y);
+}
+
+// ---------------------------------------------------------------------------------------------
 // dz = dy act'(z) and its column sums
 // ---------------------------------------------------------------------------------------------
 struct ColumnArgs {
@@ -687,8 +749,14 @@ struct ColumnArgs {
     void *db[kLinearMaxReplicas];
     uint32_t m, n, lddy, ldpre, lddz;
     uint32_t rows_per_part, parts, accumulate;
-    float *partial;                              // [replica][part][n]; NULL: no sums wanted
+    float *partial;                              // [replica][part][n]; one part: not used, the sums go straight to db
+    uint32_t want_sums, sums_f32;                // db is wanted; its type
 };
+
+template <typename O> __device__ __forceinline__ void put_sum(O *out, double s, uint32_t accumulate)
+{
+    *out = from_f32<O>((float)(accumulate ? s + (double)to_f32(*out) : s));
+}
 
 // A workgroup takes 256 columns of rows_per_part rows: eight rows at a time, eight columns a thread, the loads of U turns on their way together.
 template <typename T, int ACT>
@@ -723,7 +791,7 @@ k_columns(const ColumnArgs p)
             add8(acc, d[u]);
         }
     }
-    if (!p.partial) return;
+    if (!p.want_sums) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[r][c * 8u + j] = acc.v[j];
     __syncthreads();
@@ -732,7 +800,9 @@ k_columns(const ColumnArgs p)
     float s = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) s += sums[j][tid];
-    p.partial[((uint64_t)rep * p.parts + blockIdx.y) * p.n + col] = s;
+    if (p.parts > 1u) p.partial[((uint64_t)rep * p.parts + blockIdx.y) * p.n + col] = s;
+    else if (p.sums_f32) put_sum(static_cast<float *>(p.db[rep]) + col, (double)s, p.accumulate);
+    else put_sum(static_cast<__bf16 *>(p.db[rep]) + col, (double)s, p.accumulate);
 }
 
 // The parts of a column's sum, in fp64 and a fixed order; no parts: zero.  32 columns a workgroup, eight shares of the parts each.
@@ -752,8 +822,7 @@ k_columns_join(const ColumnArgs p)
     if (r || n >= p.n) return;
 #pragma unroll
     for (int i = 1; i < 8; ++i) s += red[i][c];
-    O *out = static_cast<O *>(p.db[rep]) + n;
-    *out = from_f32<O>((float)(p.accumulate ? s + (double)to_f32(*out) : s));
+    put_sum(static_cast<O *>(p.db[rep]) + n, s, p.accumulate);
 }
 
 struct PackArgs {

@@ -121,7 +121,7 @@ Source packed(const am_linear_config &c, const Source &s, char *to)
 struct Planned {
     double us;                   // by the measured times
     ProductPlan cut;
-    bool direct, pack_a, pack_b;
+    bool few_rows, direct, pack_a, pack_b;
     uint64_t pack_a_bytes, pack_b_bytes, partial_bytes, total;
 };
 
@@ -145,7 +145,8 @@ Planned plan_product(const am_linear_config &c, uint64_t m, uint64_t n, uint64_t
             direct_us = staged_us;
         }
     }
-    p.us = direct_us;
+    const double once_us = 3. + (bf16 ? 2. : 4.) * (double)c.replicas * ((double)m * (double)k + (double)n * (double)k + (double)m * (double)n) / 5e6;
+    p.us = direct_us > once_us ? direct_us : once_us;        // (reading and writing everything once: few rows are bound by that)
     if (p.pack_a) p.pack_a_bytes = c.replicas * packed_bytes(c, a);
     if (p.pack_b) p.pack_b_bytes = c.replicas * packed_bytes(c, b);
     if (p.cut.splits > 1) p.partial_bytes = up256(4u * p.cut.splits * c.replicas * m * n);
@@ -153,9 +154,16 @@ Planned plan_product(const am_linear_config &c, uint64_t m, uint64_t n, uint64_t
     return p;
 }
 
+constexpr uint32_t kFewRowsAtOnce = 4;       // rows of w of a workgroup
+
 Planned plan_forward(const am_linear_config &c, const am_linear_buffers &b)
 {
-    return plan_product(c, c.rows, c.out, c.in, source(c, b.x, c.rows, c.in, c.x_stride), source(c, b.w, c.out, c.in, 0));
+    Planned p = plan_product(c, c.rows, c.out, c.in, source(c, b.x, c.rows, c.in, c.x_stride), source(c, b.w, c.out, c.in, 0));
+    if (c.rows <= am_host::kFewRows && am_host::few_rows_us(c.dtype == AM_BF16, c.replicas, c.rows, c.out, c.in) < p.us) {
+        p = Planned{};
+        p.few_rows = true;
+    }
+    return p;
 }
 
 // backward: dz | column sums' parts | what the products need (dx's and dw's take turns)
@@ -177,7 +185,7 @@ PlannedBackward plan_backward(const am_linear_config &c, const am_linear_buffers
         s.dz = packed(c, s.dz, workspace);
     }
     if (b.db || s.own_dz) am_host::column_parts(c.replicas, c.rows, c.out, &s.rows_per_part, &s.parts);
-    if (b.db) s.sums_bytes = up256(4u * c.replicas * (uint64_t)s.parts * c.out);
+    if (b.db && s.parts > 1) s.sums_bytes = up256(4u * c.replicas * (uint64_t)s.parts * c.out);
     if (b.dx) s.dx = plan_product(c, c.rows, c.in, c.out, s.dz, source(c, b.w, c.out, c.in, 0));
     if (b.dw) s.dw = plan_product(c, c.out, c.in, c.rows, s.dz, source(c, b.x, c.rows, c.in, c.x_stride));
     s.total = s.dz_bytes + s.sums_bytes + (s.dx.total > s.dw.total ? s.dx.total : s.dw.total);
@@ -339,6 +347,27 @@ am_status launch_pair_shape(ProductArgs &dx, ProductArgs &dw, const Planned &p, 
     return p.cut.tile == 64 ? launch_pair<T, 64, false, 2>(dx, dw, stream) : launch_pair<T, 128, false, 2>(dx, dw, stream);
 }
 
+template <typename T, int MR>
+am_status launch_few_rows(const ProductArgs &a, hipStream_t stream)
+{
+    am::k_few_rows<T, MR, kFewRowsAtOnce><<<dim3((a.n + kFewRowsAtOnce - 1) / kFewRowsAtOnce, a.replicas), 256, 0, stream>>>(a);
+    AM_HIP(hipGetLastError());
+    return AM_OK;
+}
+
+// x w^T of a few rows (at most am_host::kFewRows), w read once by all of them
+template <typename T>
+am_status few_rows(const am_linear_config &c, const am_linear_buffers &b, ProductArgs &a, hipStream_t stream)
+{
+    for (uint32_t i = 0; i < c.replicas; ++i) { a.of[i].a = b.x[i]; a.of[i].b = b.w[i]; }
+    a.lda = (uint32_t)or_dense(c.x_stride, c.in); a.ldb = (uint32_t)c.in;
+    a.replicas = c.replicas;
+    if (a.m <= 1) return launch_few_rows<T, 1>(a, stream);
+    if (a.m <= 2) return launch_few_rows<T, 2>(a, stream);
+    if (a.m <= 4) return launch_few_rows<T, 4>(a, stream);
+    return launch_few_rows<T, 8>(a, stream);
+}
+
 template <typename T>
 am_status forward(const am_linear_config &c, const am_linear_buffers &b, const Planned &p, hipStream_t stream)
 {
@@ -354,6 +383,7 @@ am_status forward(const am_linear_config &c, const am_linear_buffers &b, const P
     a.act = c.act;
     a.ldc = (uint32_t)or_dense(c.y_stride, c.out);
     a.ldadd = (uint32_t)or_dense(c.residual_stride, c.out); a.ldpre = (uint32_t)or_dense(c.pre_stride, c.out);
+    if (p.few_rows) return few_rows<T>(c, b, a, stream);
     return launch_product<T, false, false>(c, a, p, source(c, b.x, c.rows, c.in, c.x_stride), source(c, b.w, c.out, c.in, 0), static_cast<char *>(b.workspace), stream);
 }
 
@@ -410,10 +440,11 @@ am_status backward(const am_linear_config &c, const am_linear_buffers &b, const 
         a.m = (uint32_t)c.rows; a.n = (uint32_t)c.out; a.lddz = (uint32_t)sp.dz.ld;
         a.lddy = (uint32_t)or_dense(c.y_stride, c.out); a.ldpre = (uint32_t)or_dense(c.pre_stride, c.out);
         a.rows_per_part = sp.rows_per_part; a.parts = sp.parts; a.accumulate = accumulate;
-        a.partial = b.db ? reinterpret_cast<float *>(ws + sp.dz_bytes) : nullptr;
+        a.partial = reinterpret_cast<float *>(ws + sp.dz_bytes);
+        a.want_sums = b.db != nullptr; a.sums_f32 = sizeof(O) == 4;
         const am_status s = columns<T>(a, c, stream);
         if (s != AM_OK) return s;
-        if (b.db) {
+        if (b.db && sp.parts > 1) {
             am::k_columns_join<O><<<dim3((a.n + 31u) / 32u, c.replicas), 256, 0, stream>>>(a);
             AM_HIP(hipGetLastError());
         }

@@ -84,14 +84,26 @@ inline bool pair_plan(bool bf16, bool direct, uint64_t replicas, const Extent &a
     return found;
 }
 
+// Time of x w^T with every weight read once by a workgroup that takes all rows of x, up to eight: reading w, at 6 TB/s for one row, and
+// more the more rows share a weight (8 x 2048 x 8192 in bf16: 42, 48, 76 and 158 us for 1, 2, 4 and 8 rows; tiles 41; 5110 x 3456 in fp32:
+// 12.6, 13, 15 and 24; tiles 35).
+constexpr uint64_t kFewRows = 8;
+inline double few_rows_us(bool bf16, uint64_t replicas, uint64_t m, uint64_t n, uint64_t k)
+{
+    static const double bf16_share[4] = {1., 1.3, 1.8, 3.8}, f32_share[4] = {1., 1.05, 1.25, 2.};
+    const int i = m <= 1 ? 0 : m <= 2 ? 1 : m <= 4 ? 2 : 3;
+    return 3. + (double)(replicas * n) * (double)k * (bf16 ? 2. * bf16_share[i] : 4. * f32_share[i]) / 6e6;
+}
+
 // Time of copying an operand to aligned rows first: a launch, and both ways at what a copy of strided rows reaches.
 inline double pack_us(uint64_t bytes) { return 3.5 + 2. * (double)bytes / 4e6; }
 
-// Rows for each workgroup of the column sums: some 4096 workgroups, 32 rows (one turn) at least.
+// Rows for each workgroup of the column sums: some 4096 workgroups, 32 rows (one turn) at least.  Up to 64 rows one workgroup takes a column's
+// all, which saves a launch (256 rows: 33 us for 29 of a small backward call).
 inline void column_parts(uint64_t replicas, uint64_t m, uint64_t n, uint32_t *rows_per_part, uint32_t *parts)
 {
     const uint64_t across = ((n + 255) / 256) * replicas;
-    const uint64_t want = across >= 4096 ? 1 : 4096 / across;
+    const uint64_t want = across >= 4096 || m <= 64 ? 1 : 4096 / across;
     uint64_t rows = ((m + want - 1) / want + 31) / 32 * 32;
     if ((m + rows - 1) / rows > 65535) rows = (m + 65534) / 65535;
     *rows_per_part = (uint32_t)rows;

@@ -63,12 +63,20 @@ for _f in (lib.am_grad_norm, lib.am_clip_grads):
     _f.argtypes = [C.POINTER(NormConfig), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
 
 
+# The checks below run several times in a call of some ten microseconds, so they ask each question once and keep the messages apart.
+_Tensor, _empty = torch.Tensor, torch.empty
+_raw_stream = torch._C._cuda_getCurrentRawStream           # (torch.cuda.current_stream makes an object of it: 2 us)
+
+
 def _replicas(name, tensors, count=None):
-    tensors = list(tensors)
-    if not 1 <= len(tensors) <= MAX_REPLICAS:
-        raise ValueError(f"{name}: {len(tensors)} tensors, 1 to {MAX_REPLICAS} replicas expected")
-    if count is not None and len(tensors) != count:
-        raise ValueError(f"{name}: {len(tensors)} tensors for {count} replicas")
+    if type(tensors) is not list:
+        tensors = list(tensors)
+    n = len(tensors)
+    if n != count:
+        if count is not None:
+            raise ValueError(f"{name}: {n} tensors for {count} replicas")
+        if not 1 <= n <= MAX_REPLICAS:
+            raise ValueError(f"{name}: {n} tensors, 1 to {MAX_REPLICAS} replicas expected")
     return tensors
 
 
@@ -77,22 +85,31 @@ def _refuse(name, i, t, shape, dtype, device):
     raise ValueError(f"{name}[{i}] must be a {dtype} tensor of shape {shape} on {device}, got {got}")
 
 
-def _matching(name, tensors, shape, dtype, device, dense=False):
-    """The raw pointers are all the C side sees: what could make a kernel read past an allocation is refused here.  Returns
-    the row stride that all replicas share (0: rows are dense)."""
+def _dense(name, tensors, shape, dtype, device):
+    """The raw pointers are all the C side sees: what could make a kernel read past an allocation is refused here and in _rows."""
+    for i, t in enumerate(tensors):
+        if not isinstance(t, _Tensor) or t.shape != shape or t.dtype != dtype or t.device != device:
+            _refuse(name, i, t, shape, dtype, device)
+        if not t.is_contiguous():
+            raise ValueError(f"{name}[{i}] has strides {t.stride()}: it must be contiguous")
+
+
+def _rows(name, tensors, shape, dtype, device):
+    """[rows, columns] tensors whose rows may lie apart; returns the stride that all replicas share (0: rows are dense)."""
     stride = None
     for i, t in enumerate(tensors):
-        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.device != device:
+        if not isinstance(t, _Tensor) or t.shape != shape or t.dtype != dtype or t.device != device:
             _refuse(name, i, t, shape, dtype, device)
         if t.is_contiguous():
             row = 0
-        elif dense or len(shape) != 2 or (shape[1] > 1 and t.stride(1) != 1) or (shape[0] > 1 and t.stride(0) < shape[1]):
-            raise ValueError(f"{name}[{i}] has strides {t.stride()}: " + ("it must be contiguous" if dense else "rows must be dense and not overlap"))
+        elif (shape[1] > 1 and t.stride(1) != 1) or (shape[0] > 1 and t.stride(0) < shape[1]):
+            raise ValueError(f"{name}[{i}] has strides {t.stride()}: rows must be dense and not overlap")
         else:
             row = t.stride(0) if shape[0] > 1 else 0
-        if stride is not None and row != stride:
-            raise ValueError(f"{name}: all replicas must have the same row stride")
-        stride = row
+        if row != stride:
+            if stride is not None:
+                raise ValueError(f"{name}: all replicas must have the same row stride")
+            stride = row
     return stride
 
 
@@ -115,25 +132,31 @@ def _fill(buf, R, tables):
 
 
 def _workspace(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    return _empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _current(device):
+    """Whether `device` is the current one (else the call is made within torch.cuda.device)."""
+    return device.index == torch.cuda.current_device()
 
 
 def _linear_call(cfg, tables, backward, accumulate, device):
+    if not _current(device):
+        with torch.cuda.device(device):
+            return _linear_call(cfg, tables, backward, accumulate, device)
     buf = LinearBuffers()
-    keep = _fill(buf, cfg.replicas, tables)
+    keep = _fill(buf, cfg.replicas, tables)               # noqa: F841 (the tables live as long as the call)
+    refs, stream = (C.byref(cfg), C.byref(buf)), _raw_stream(device.index)
+    call = (lambda: lib.am_linear_backward(*refs, accumulate, stream)) if backward else (lambda: lib.am_linear(*refs, stream))
+    # Most small calls need no workspace; one that does is refused before anything is enqueued, and made again with what it asks for.
+    if call() == 0:
+        return
     need = C.c_uint64()
-    cfg_ref, buf_ref = C.byref(cfg), C.byref(buf)
-    with _on(device):
-        _check(lib.am_linear_workspace(cfg_ref, buf_ref, backward, C.byref(need)))
-        if need.value:
-            space = _workspace(need.value, device)
-            buf.workspace, buf.workspace_bytes = space.data_ptr(), need.value
-        stream = torch.cuda.current_stream(device).cuda_stream
-        if backward:
-            _check(lib.am_linear_backward(cfg_ref, buf_ref, accumulate, stream))
-        else:
-            _check(lib.am_linear(cfg_ref, buf_ref, stream))
-    del keep
+    _check(lib.am_linear_workspace(*refs, backward, C.byref(need)))
+    if need.value:
+        space = _workspace(need.value, device)
+        buf.workspace, buf.workspace_bytes = space.data_ptr(), need.value
+    _check(call())
 
 
 def _check_product(x, w):
@@ -147,8 +170,8 @@ def _check_product(x, w):
     if width == 0 or out == 0:
         raise ValueError(f"a product of {width} by {out} columns")
     dtype = x[0].dtype
-    x_stride = _matching("x", x, (rows, width), dtype, device)
-    _matching("w", w, (out, width), dtype, device, dense=True)
+    x_stride = _rows("x", x, (rows, width), dtype, device)
+    _dense("w", w, (out, width), dtype, device)
     return x, w, device, dtype, rows, width, out, x_stride
 
 
@@ -162,13 +185,13 @@ def linear(x, w, bias=None, act=ACT_NONE, residual=None, with_pre=False):
     cfg = LinearConfig(R, code, code, act, rows, width, out, x_stride)
     if bias is not None:
         tables["bias"] = bias = _replicas("bias", bias, R)
-        _matching("bias", bias, (out,), dtype, device, dense=True)
+        _dense("bias", bias, (out,), dtype, device)
     if residual is not None:
         tables["residual"] = residual = _replicas("residual", residual, R)
-        cfg.residual_stride = _matching("residual", residual, (rows, out), dtype, device)
-    tables["y"] = y = [torch.empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
+        cfg.residual_stride = _rows("residual", residual, (rows, out), dtype, device)
+    tables["y"] = y = [_empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
     if with_pre:
-        tables["pre"] = pre = [torch.empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
+        tables["pre"] = pre = [_empty((rows, out), dtype=dtype, device=device) for _ in range(R)]
     _linear_call(cfg, tables, 0, 0, device)
     return (y, pre) if with_pre else y
 
@@ -182,13 +205,13 @@ def linear_backward(dy, x, w, act=ACT_NONE, pre=None, dw=None, db=None, accumula
     if not (need_dx or dw is not None or db is not None):
         raise ValueError("no gradient is wanted: need_dx is off, dw and db are None")
     dy = _replicas("dy", dy, R)
-    cfg = LinearConfig(R, code, code, act, rows, width, out, x_stride, _matching("dy", dy, (rows, out), dtype, device))
+    cfg = LinearConfig(R, code, code, act, rows, width, out, x_stride, _rows("dy", dy, (rows, out), dtype, device))
     tables = {"dy": dy, "x": x, "w": w}
     if act != ACT_NONE:
         if pre is None:
             raise ValueError("the gradient of an activation needs pre")
         tables["pre"] = pre = _replicas("pre", pre, R)
-        cfg.pre_stride = _matching("pre", pre, (rows, out), dtype, device)
+        cfg.pre_stride = _rows("pre", pre, (rows, out), dtype, device)
     grad_dtype = None
     for name, grads, shape in (("dw", dw, (out, width)), ("db", db, (out,))):
         if grads is None:
@@ -197,10 +220,10 @@ def linear_backward(dy, x, w, act=ACT_NONE, pre=None, dw=None, db=None, accumula
         if grad_dtype is None:
             grad_dtype = _grad_type(name, grads[0], dtype)
             cfg.grad_dtype = _DTYPES[grad_dtype]
-        _matching(name, grads, shape, grad_dtype, device, dense=True)
+        _dense(name, grads, shape, grad_dtype, device)
     dx = None
     if need_dx:
-        tables["dx"] = dx = [torch.empty((rows, width), dtype=dtype, device=device) for _ in range(R)]
+        tables["dx"] = dx = [_empty((rows, width), dtype=dtype, device=device) for _ in range(R)]
     _linear_call(cfg, tables, 1, int(accumulate), device)
     return dx
 
@@ -244,14 +267,14 @@ def _norm_call(entry, grads, max_norm, out):
     codes = array("I", [_DTYPES[t] for t in kinds])
     outs = None if out is None else array("Q", [t.data_ptr() for t in out])
     cfg = NormConfig(R, count, sizes.buffer_info()[0], codes.buffer_info()[0], out_dtype, max_norm)
-    result = torch.empty(2, R, dtype=torch.float32, device=device)
+    result = _empty(2, R, dtype=torch.float32, device=device)
     need = C.c_uint64()
     with _on(device):
         _check(lib.am_norm_workspace(C.byref(cfg), C.byref(need)))
         space = _workspace(need.value, device)
         at = result.data_ptr()
-        _check(entry(C.byref(cfg), pointers.buffer_info()[0], None if outs is None else outs.buffer_info()[0], at, at + 4 * R, None if space is None else space.data_ptr(), need.value,
-                     torch.cuda.current_stream(device).cuda_stream))
+        _check(entry(C.byref(cfg), pointers.buffer_info()[0], None if outs is None else outs.buffer_info()[0], at, at + 4 * R,
+                     None if space is None else space.data_ptr(), need.value, _raw_stream(device.index)))
     return result[0], result[1]
 
 
@@ -305,16 +328,16 @@ def _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
     k_shape = torch.Size((tokens, k[0].shape[1], dim))
     q_stride, k_stride = _heads("q", q, q_shape, dtype, device), _heads("k", k, k_shape, dtype, device)
     q_gain, k_gain = _replicas("q_gain", q_gain, R), _replicas("k_gain", k_gain, R)
-    _matching("q_gain", q_gain, (dim,), dtype, device, dense=True)
-    _matching("k_gain", k_gain, (dim,), dtype, device, dense=True)
+    _dense("q_gain", q_gain, (dim,), dtype, device)
+    _dense("k_gain", k_gain, (dim,), dtype, device)
     if not (isinstance(cos, torch.Tensor) and isinstance(sin, torch.Tensor) and cos.dim() == 2 and cos.shape == sin.shape):
         raise ValueError("cos and sin must be tensors of one shape [rows, rotated / 2]")
-    _matching("cos, sin", (cos, sin), cos.shape, torch.float32, device, dense=True)
+    _dense("cos, sin", (cos, sin), cos.shape, torch.float32, device)
     cfg = QkConfig(R, _DTYPES[dtype], _DTYPES[dtype], 1 if interleaved else 0, tokens, q_heads, k_shape[1], dim, 2 * cos.shape[1], q_stride, k_stride, cos.shape[0], eps)
     tables = {"q": q, "k": k, "q_gain": q_gain, "k_gain": k_gain}
     if positions is not None:
         tables["positions"] = positions = _replicas("positions", positions, R)
-        _matching("positions", positions, (tokens,), torch.int32, device, dense=True)
+        _dense("positions", positions, (tokens,), torch.int32, device)
     buf = QkBuffers()
     buf.cos, buf.sin = cos.data_ptr(), sin.data_ptr()
     return cfg, buf, tables, device, dtype, q_shape, k_shape
@@ -328,11 +351,11 @@ def qk_norm(q, k, q_gain, k_gain, cos, sin, positions=None, eps=1e-6, interleave
     have makes the token's rotated elements NaN.  Returns two lists of dense tensors."""
     cfg, buf, tables, device, dtype, q_shape, k_shape = _qk_call(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
     R = cfg.replicas
-    tables["q_out"] = q_out = [torch.empty(q_shape, dtype=dtype, device=device) for _ in range(R)]
-    tables["k_out"] = k_out = [torch.empty(k_shape, dtype=dtype, device=device) for _ in range(R)]
+    tables["q_out"] = q_out = [_empty(q_shape, dtype=dtype, device=device) for _ in range(R)]
+    tables["k_out"] = k_out = [_empty(k_shape, dtype=dtype, device=device) for _ in range(R)]
     keep = _fill(buf, R, tables)
     with _on(device):
-        _check(lib.am_qk_norm(C.byref(cfg), C.byref(buf), torch.cuda.current_stream(device).cuda_stream))
+        _check(lib.am_qk_norm(C.byref(cfg), C.byref(buf), _raw_stream(device.index)))
     del keep
     return q_out, k_out
 
@@ -353,9 +376,9 @@ def qk_norm_backward(dq, dk, q, k, q_gain, k_gain, cos, sin, positions=None, eps
         if grad_dtype is None:
             grad_dtype = _grad_type(name, grads[0], dtype)
             cfg.grad_dtype = _DTYPES[grad_dtype]
-        _matching(name, grads, (q_shape[2],), grad_dtype, device, dense=True)
-    tables["dq"] = q_grad = [torch.empty(q_shape, dtype=dtype, device=device) for _ in range(R)]
-    tables["dk"] = k_grad = [torch.empty(k_shape, dtype=dtype, device=device) for _ in range(R)]
+        _dense(name, grads, (q_shape[2],), grad_dtype, device)
+    tables["dq"] = q_grad = [_empty(q_shape, dtype=dtype, device=device) for _ in range(R)]
+    tables["dk"] = k_grad = [_empty(k_shape, dtype=dtype, device=device) for _ in range(R)]
     keep = _fill(buf, R, tables)
     need = C.c_uint64()
     with _on(device):
@@ -363,6 +386,6 @@ def qk_norm_backward(dq, dk, q, k, q_gain, k_gain, cos, sin, positions=None, eps
         if need.value:
             space = _workspace(need.value, device)
             buf.workspace, buf.workspace_bytes = space.data_ptr(), need.value
-        _check(lib.am_qk_norm_backward(C.byref(cfg), C.byref(buf), int(accumulate), torch.cuda.current_stream(device).cuda_stream))
+        _check(lib.am_qk_norm_backward(C.byref(cfg), C.byref(buf), int(accumulate), _raw_stream(device.index)))
     del keep
     return q_grad, k_grad

@@ -124,6 +124,15 @@ def test_operands_that_are_moved_to_aligned_rows_first(amlib, M, K, N, shift):
         _backward_case(amlib, dtype, torch.float32, 1, M, K, N, "RELU", pad=1, shift=shift, seed=8)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 8, 9])
+def test_few_rows(amlib, dtype, M):
+    """Where every weight is read once for all rows, at widths that are no multiples of what a workgroup takes."""
+    _forward_case(amlib, dtype, 2, M, 4097, 261, "GELU", True, True, True, pad=1, shift=3, seed=9)
+    _forward_case(amlib, dtype, 1, M, 2048, 1024, "NONE", False, False, False, seed=10)
+    _forward_case(amlib, dtype, 3, M, 5, 3, "SILU", True, False, True, seed=11)
+
+
 def _backward_case(am, dtype, grad_dtype, R, M, K, N, act, bias=True, accumulate=False, need_dx=True, need_dw=True, pad=0, shift=0, seed=0):
     print("linear_backward", dtype, grad_dtype, R, M, K, N, act, bias, accumulate, need_dx, need_dw, pad, shift, flush=True)
     gen = torch.Generator().manual_seed(seed)
