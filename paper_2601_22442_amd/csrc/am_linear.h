@@ -536,26 +536,13 @@ k_product(const ProductArgs p)
     product_tile<T, BM, BN, WM, WN, A_ACROSS, B_ACROSS, DIRECT, STAGES>(p, blockIdx.x, gridDim.x, lds);
 }
 
-// The two products of a backward call, which need nothing of each other, in one launch: together they leave fewer compute units
-// without work in the last round, and one launch less.  Workgroups below `first` take dz w (dw_first: dz^T x), the others the other.
-template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int STAGES>
-__global__ void __launch_bounds__(64 * WM * WN, 2)
-k_product_pair(const ProductArgs dx, const ProductArgs dw, uint32_t first, uint32_t dw_first)
-{
-    extern __shared__ __align__(16) char lds[];
-    const bool low = blockIdx.x < first;
-    const uint32_t block = low ? blockIdx.x : blockIdx.x - first, blocks = low ? first : gridDim.x - first;
-    if (low != (dw_first != 0u)) product_tile<T, BM, BN, WM, WN, false, true, DIRECT, STAGES>(dx, block, blocks, lds);
-    else product_tile<T, BM, BN, WM, WN, true, true, DIRECT, STAGES>(dw, block, blocks, lds);
-}
-
-// The 256 x 256 tile of bf16: eight waves of 128 x 64, two to a SIMD.  Steps of 128 bytes of k (whole
-// lines of memory) in two halves of LDS.  A wave's stream never stops for LDS: while it multiplies the fragments of one half step it
+// The larger tiles of bf16 straight from memory: 256 x 256 in eight waves of 128 x 64, 128 x 128 in four of 64 x 64 (two workgroups a compute
+// unit); two waves to a SIMD either way.  Steps of 128 bytes of k (whole lines of memory) in two halves of LDS.  A wave's stream never stops for LDS: while it multiplies the fragments of one half step it
 // reads those of the next.  Step t's halves are h0, h1:
 //   products (t, h0), meanwhile read (t, h1);
 //   wait until step t + 1 has come and own reads of step t are done, barrier: nobody reads step t any more, all of step t + 1 is there;
 //   products (t, h1), meanwhile set out step t + 2 over step t and read (t + 1, h0).
-// So 64 KB are on their way at any time, for the length of a step.  Steps past the end set out zeros and are read but not multiplied.
+// So a step is on its way at any time, for the length of one: 64 KB a compute unit.  Steps past the end set out zeros and are read but not multiplied.
 __device__ __forceinline__ void meet()                                  // all waves' LDS reads and direct loads before here are done for all
 {
     __builtin_amdgcn_sched_barrier(0);
@@ -572,16 +559,16 @@ __device__ __forceinline__ void fetch_half(const char *__restrict__ from, int h,
     for (int i = 0; i < MF; ++i) fa[i] = A::fragment(from, wm, i, h, lane);
 }
 
-// The order in which a half step's 32 products, its LDS reads (two for a turned fragment) and, in the second half, 8 direct loads are
-// issued: four products at a time with reads and a load between them, so that each finds the matrix unit busy; the last eight
-// products cover the last reads' way.
-template <int READS, bool LOADS, int G = 0>
+// The order in which a half step's products, its LDS reads (two for a turned fragment) and, in the second half, 8 direct loads are
+// issued: an eighth of the products at a time with reads and a load between them, so that each finds the matrix unit busy; the last quarter
+// of the products covers the last reads' way.
+template <int PRODUCTS, int READS, bool LOADS, int G = 0>
 __device__ __forceinline__ void interleave()
 {
-    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / 8, 0);
     if constexpr (LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     if constexpr (G < 6) __builtin_amdgcn_sched_group_barrier(0x100, READS * (G + 1) / 6 - READS * G / 6, 0);
-    if constexpr (G < 7) interleave<READS, LOADS, G + 1>();
+    if constexpr (G < 7) interleave<PRODUCTS, READS, LOADS, G + 1>();
 }
 
 // `over` is written by direct loads while `from` is read
@@ -594,24 +581,24 @@ __device__ __forceinline__ void second_half(const char *__restrict__ from, char 
     b.template direct<FULL>(over + A::kBytes, ob, k0, kb, wave, lane);
     fetch_half<T, A, B, MF, NF>(from, 0, na, nb, wm, wn, lane);
     multiply_half<T, MF, NF>(fa, fb, acc);
-    interleave<MF * (A::kAcross ? 2 : 1) + NF * (B::kAcross ? 2 : 1), true>();
+    interleave<MF * NF, MF * (A::kAcross ? 2 : 1) + NF * (B::kAcross ? 2 : 1), true>();
 }
 
-template <bool A_ACROSS, bool B_ACROSS>
-__global__ void __launch_bounds__(512, 2)
-k_product_large(const ProductArgs p)
+// STREAM: the result goes past the caches.
+template <int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, bool STREAM>
+__device__ __forceinline__ void ahead_tile(const ProductArgs &p, uint32_t block, uint32_t blocks, char *lds)
 {
     typedef __bf16 T;
-    constexpr int BM = 256, BN = 256, NT = 512, MF = 8, NF = 4;
+    constexpr int NT = 64 * WM * WN, MF = BM / WM / 16, NF = BN / WN / 16;
     using A = Operand<T, BM, NT, A_ACROSS, 8>;
     using B = Operand<T, BN, NT, B_ACROSS, 8>;
     constexpr int kStep = A::kStep, kStage = A::kBytes + B::kBytes;
-    extern __shared__ __align__(16) char lds[];
+    static_assert(A::kPerThread + B::kPerThread == 8, "as interleave has them");
 
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Where w = where(p, blockIdx.x, gridDim.x);
+    const Where w = where(p, block, blocks);
     const uint32_t m0 = w.tile_m * BM, n0 = w.tile_n * BN;
-    const int wm = wave / 4 * 128, wn = wave % 4 * 64;
+    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
     const uint32_t k_first = w.split * p.split_k;
     const uint32_t k_end = p.k - k_first < p.split_k ? p.k : k_first + p.split_k;
     const int steps = (int)((k_end - k_first + kStep - 1) / kStep);
@@ -648,7 +635,7 @@ k_product_large(const ProductArgs p)
         char *cur = lds + (t & 1) * kStage, *next = lds + ((t + 1) & 1) * kStage;
         fetch_half<T, A, B, MF, NF>(cur, 1, fa1, fb1, wm, wn, lane);
         multiply_half<T, MF, NF>(fa0, fb0, acc);
-        interleave<MF * (A_ACROSS ? 2 : 1) + NF * (B_ACROSS ? 2 : 1), false>();
+        interleave<MF * NF, MF * (A_ACROSS ? 2 : 1) + NF * (B_ACROSS ? 2 : 1), false>();
         meet();
         second_half<T, A, B, MF, NF, decltype(full)::value>(next, cur, a, b, oa, ob, start(t + 2), left(t + 2, A_ACROSS), left(t + 2, B_ACROSS), fa1, fb1, fa0, fb0, acc, wm, wn, wave, lane);
         __builtin_amdgcn_sched_barrier(0);
@@ -657,7 +644,45 @@ k_product_large(const ProductArgs p)
     for (; t < steps; ++t) step(std::false_type{});
     wait_loads<0>();
     __syncthreads();
-    finish_wave<T, 128, 64, true>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
+    finish_wave<T, BM / WM, BN / WN, STREAM>(p, w, acc, lds, m0 + (uint32_t)wm, n0 + (uint32_t)wn, wave, lane);
+}
+
+template <bool A_ACROSS, bool B_ACROSS>
+__global__ void __launch_bounds__(512, 2)
+k_product_large(const ProductArgs p)
+{
+    extern __shared__ __align__(16) char lds[];
+    ahead_tile<256, 256, 2, 4, A_ACROSS, B_ACROSS, true>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// From kAheadSteps steps on; fewer do not repay the second step's way and what is read ahead in vain (k_product: 3 % faster below six
+// steps, the same at ten, 4 to 9 % slower from twelve on).
+constexpr uint32_t kAheadSteps = 12;
+template <bool A_ACROSS, bool B_ACROSS>
+__global__ void __launch_bounds__(256, 2)
+k_product_medium(const ProductArgs p)
+{
+    extern __shared__ __align__(16) char lds[];
+    ahead_tile<128, 128, 2, 2, A_ACROSS, B_ACROSS, false>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// The two products of a backward call, which need nothing of each other, in one launch: together they leave fewer compute units
+// without work in the last round, and one launch less.  Workgroups below `first` take dz w (dw_first: dz^T x), the others the other.
+// AHEAD: by ahead_tile.
+template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int STAGES, bool AHEAD>
+__global__ void __launch_bounds__(64 * WM * WN, 2)
+k_product_pair(const ProductArgs dx, const ProductArgs dw, uint32_t first, uint32_t dw_first)
+{
+    extern __shared__ __align__(16) char lds[];
+    const bool low = blockIdx.x < first;
+    const uint32_t block = low ? blockIdx.x : blockIdx.x - first, blocks = low ? first : gridDim.x - first;
+    if constexpr (AHEAD) {
+        if (low != (dw_first != 0u)) ahead_tile<BM, BN, WM, WN, false, true, false>(dx, block, blocks, lds);
+        else ahead_tile<BM, BN, WM, WN, true, true, false>(dw, block, blocks, lds);
+    } else {
+        if (low != (dw_first != 0u)) product_tile<T, BM, BN, WM, WN, false, true, DIRECT, STAGES>(dx, block, blocks, lds);
+        else product_tile<T, BM, BN, WM, WN, true, true, DIRECT, STAGES>(dw, block, blocks, lds);
+    }
 }
 
 // The parts of k that workgroups summed apart, joined in their order, and the epilogue.
@@ -763,7 +788,7 @@ template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 k_columns(const ColumnArgs p)
 {
-    constexpr int U = sizeof(T) == 2 ? 4 : 2;
+    constexpr int U = 2;
     __shared__ float sums[8][256];
     const uint32_t rep = blockIdx.z, tid = threadIdx.x, c = tid & 31u, r = tid >> 5;
     const uint32_t n = blockIdx.x * 256u + c * 8u;

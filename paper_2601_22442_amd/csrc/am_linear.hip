@@ -247,6 +247,8 @@ am_status launch_tiles(ProductArgs &a, hipStream_t stream)
     return launch_kernel(am::k_product<T, BM, BN, WM, WN, AA, BA, DIRECT, STAGES>, a, BM, 64 * WM * WN, (uint32_t)STAGES * (BM + BN) * 128u, stream);
 }
 
+bool many_steps(const ProductPlan &p) { return p.split_k >= 64u * am::kAheadSteps; }      // (bf16: 64 k a step)
+
 template <typename T, bool AA, bool BA, bool DIRECT>
 am_status launch_shape(ProductArgs &a, const ProductPlan &p, hipStream_t stream)
 {
@@ -259,6 +261,8 @@ am_status launch_shape(ProductArgs &a, const ProductPlan &p, hipStream_t stream)
     if constexpr (DIRECT)
         if (p.tile == 64 && p.stages == 4) return launch_tiles<T, 64, 64, 2, 2, AA, BA, DIRECT, 4>(a, stream);
     if (p.tile == 64) return launch_tiles<T, 64, 64, 2, 2, AA, BA, DIRECT, 2>(a, stream);
+    if constexpr (DIRECT && sizeof(T) == 2)
+        if (many_steps(p)) return launch_kernel(am::k_product_medium<AA, BA>, a, 128, 256, 65536, stream);
     return launch_tiles<T, 128, 128, 2, 2, AA, BA, DIRECT, 2>(a, stream);
 }
 
@@ -320,7 +324,7 @@ am_status launch_product(const am_linear_config &c, ProductArgs &args, const Pla
 }
 
 // dx and dw in one launch, the one with the longer sums first
-template <typename T, int TILE, bool DIRECT, int STAGES>
+template <typename T, int TILE, bool DIRECT, int STAGES, bool AHEAD = false>
 am_status launch_pair(ProductArgs &dx, ProductArgs &dw, hipStream_t stream)
 {
     uint64_t blocks[2];
@@ -332,16 +336,18 @@ am_status launch_pair(ProductArgs &dx, ProductArgs &dw, hipStream_t stream)
     }
     if (blocks[0] + blocks[1] >= kMaxExtent) return fail(AM_EINVAL, "products of %llu tiles are too large for one launch", (unsigned long long)(blocks[0] + blocks[1]));
     const uint32_t dw_first = dw.k > dx.k, first = (uint32_t)blocks[dw_first];
-    am::k_product_pair<T, TILE, TILE, 2, 2, DIRECT, STAGES><<<(uint32_t)(blocks[0] + blocks[1]), 256, STAGES * 2u * TILE * 128u, stream>>>(dx, dw, first, dw_first);
+    am::k_product_pair<T, TILE, TILE, 2, 2, DIRECT, STAGES, AHEAD><<<(uint32_t)(blocks[0] + blocks[1]), 256, STAGES * 2u * TILE * 128u, stream>>>(dx, dw, first, dw_first);
     AM_HIP(hipGetLastError());
     return AM_OK;
 }
 
 template <typename T>
-am_status launch_pair_shape(ProductArgs &dx, ProductArgs &dw, const Planned &p, hipStream_t stream)
+am_status launch_pair_shape(ProductArgs &dx, ProductArgs &dw, const Planned &p, const Planned &pw, hipStream_t stream)
 {
     if (p.direct) {
         if (p.cut.tile == 64) return p.cut.stages == 4 ? launch_pair<T, 64, true, 4>(dx, dw, stream) : launch_pair<T, 64, true, 2>(dx, dw, stream);
+        if constexpr (sizeof(T) == 2)
+            if (many_steps(p.cut) && many_steps(pw.cut)) return launch_pair<T, 128, true, 2, true>(dx, dw, stream);
         return launch_pair<T, 128, true, 2>(dx, dw, stream);
     }
     return p.cut.tile == 64 ? launch_pair<T, 64, false, 2>(dx, dw, stream) : launch_pair<T, 128, false, 2>(dx, dw, stream);
@@ -468,7 +474,7 @@ am_status backward(const am_linear_config &c, const am_linear_buffers &b, const 
     if (sp.pair) {
         s = set_operands<T, false, true>(c, dx, sp.dx, sp.dz, w, space, stream);
         if (s == AM_OK) s = set_operands<T, true, true>(c, dw, sp.dw, sp.dz, x, space + sp.dx.total, stream);
-        return s == AM_OK ? launch_pair_shape<T>(dx, dw, sp.dx, stream) : s;
+        return s == AM_OK ? launch_pair_shape<T>(dx, dw, sp.dx, sp.dw, stream) : s;
     }
     if (b.dx) s = launch_product<T, false, true>(c, dx, sp.dx, sp.dz, w, space, stream);
     if (b.dw && s == AM_OK) s = launch_product<T, true, true>(c, dw, sp.dw, sp.dz, x, space, stream);

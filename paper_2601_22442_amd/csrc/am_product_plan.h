@@ -17,13 +17,13 @@ struct ProductPlan {
 // `share_us` for each workgroup of its compute unit where that is longer; `resident` of them run at a time; every workgroup costs `fixed_us` besides; a sum
 // that is split costs a launch, the host's 2 us for it and its parts' way through memory.  The constants fit 3900 timed products on an MI355X (16 to
 // 8192 rows, 128 to 8192 columns, one to eight replicas, 1 to 32 splits; straight into LDS and through registers): what the rule
-// picks took 0.4 % (bf16) and 2.5 % (fp32) more than the best of all on average, 20 % at worst (10.5 us against 8.7); through registers 3 to 5 %.
+// picks took 1.5 % (bf16) and 2.5 % (fp32) more than the best of all on average, 20 % at worst (10.5 us against 8.7); through registers 3 to 5 %.
 struct TileCost { uint32_t tile, stages, resident; double alone_us, share_us, fixed_us; };
 struct ProductCost { TileCost tiles[4]; uint32_t count; double join_us, join_tb_s; };
 
 inline const ProductCost &product_cost(bool bf16, bool direct)
 {
-    static const ProductCost bf16_direct = {{{256, 2, 1, 1.17, 1.17, 6.58}, {128, 2, 2, 0.587, 0.461, 3.64}, {64, 2, 4, 0.305, 0.189, 2.42}, {64, 4, 2, 0.18, 0.179, 2.68}}, 4, 4.9, 4.25};
+    static const ProductCost bf16_direct = {{{256, 2, 1, 1.16, 1.16, 6.2}, {128, 2, 2, 0.56, 0.44, 3.2}, {64, 2, 4, 0.33, 0.19, 2.1}, {64, 4, 2, 0.2, 0.165, 2.5}}, 4, 5.0, 4.1};
     static const ProductCost bf16_staged = {{{256, 2, 1, 2.2, 2.2, 4.5}, {128, 2, 2, 1.0, 0.75, 3.3}, {64, 2, 4, 0.62, 0.28, 1.4}}, 3, 5.5, 3.3};
     static const ProductCost f32_direct = {{{128, 2, 2, 1.99, 1.99, 4.5}, {64, 2, 4, 0.691, 0.57, 2.28}, {64, 4, 2, 0.558, 0.558, 2.6}}, 3, 5.85, 4.8};
     static const ProductCost f32_staged = {{{128, 2, 2, 2.34, 2.12, 4.4}, {64, 2, 4, 0.752, 0.619, 2.5}}, 2, 5.6, 4.85};

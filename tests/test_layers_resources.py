@@ -11,7 +11,7 @@ FLAGS = [f for f in HIPCC_FLAGS if f not in ("-shared", "-Wall", "-Wextra")]
 # name, vector registers that the resident waves leave: two waves a SIMD with 256, four with 128
 LARGE = [(f"am::k_product_large<{a}, {b}>", 256) for a, b in (("false", "false"), ("false", "true"), ("true", "true"))]
 SMALL = [(f"am::k_product<__bf16, 64, 64, 2, 2, {a}, {b}, true, {s}>", 128) for a, b in (("false", "false"), ("true", "true")) for s in (2, 4)]
-MEDIUM = [("am::k_product<__bf16, 128, 128, 2, 2, false, true, true, 2>", 256)]
+MEDIUM = [("am::k_product<__bf16, 128, 128, 2, 2, false, true, true, 2>", 256), ("am::k_product_medium<true, true>", 256)]
 
 
 @pytest.fixture(scope="module")
