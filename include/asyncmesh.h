@@ -345,7 +345,8 @@ am_status am_linear_workspace(const am_linear_config *cfg, const am_linear_buffe
 am_status am_linear(const am_linear_config *cfg, const am_linear_buffers *buf, void *hip_stream);
 
 /* The gradients: dz = dy act'(z), dx = dz w, dw = dz^T x, db = column sums of dz.  act' is that of the stored z (relu' (0) = 0);
- * with an activation, dz is rounded to dtype before the two products (db sums it unrounded).  accumulate != 0: dw and db are
+ * with an activation, dz is rounded to dtype before the two products (db sums it unrounded).  So with AM_BF16 and gelu or silu, dx and dw
+ * are those of a dz in bf16 also where dw is fp32: dw's relative error is then about 0.0017 (its sums are fp32 all the same).  accumulate != 0: dw and db are
  * added to what is there (micro-batches), the sum rounded once.  The residual's gradient is dy itself. */
 am_status am_linear_backward(const am_linear_config *cfg, const am_linear_buffers *buf, int accumulate, void *hip_stream);
 

@@ -1,5 +1,6 @@
 """MI355X-native AsyncMesh stage update: fused optimizer step + look-ahead + asynchronous sparse
-averaging with EMA delay correction, as a C-ABI HIP library with a thin binding.
+averaging with EMA delay correction, as a C-ABI HIP library with a thin binding; and the layers that own
+a stage's parameters with the gradient norm that clips them (layers.py).
 
 The binding (and with it the built library) is loaded on first use of one of its names, so that
 `paper_2601_22442_amd.build` can be imported in a tree where nothing is built yet.  There is no

